@@ -279,6 +279,155 @@ spec_status_t spec_advance(const void* hidden, int32_t hidden_dtype, int32_t bat
                            int32_t emb_dim, const int32_t* best_cand, const int32_t* accept_len,
                            const int32_t* out_tokens, void* next_state, int32_t* next_tok, void* hip_stream);
 
+/* ---- around the base model's forward over the token tree ---------------------------------------------------
+ * A step of a base model that evaluates the tree of spec_tree_metadata (Sec. 3.1: all candidates at once, every shared
+ * prefix once) has, per sequence, ROWS: row 0 is the token sampled last, row 1 + i is node i, R = 1 + M rows with
+ * M >= 0 node slots per sequence (M = 0: plain decoding).  With ctx_len[q] tokens of sequence q in the cache, row 0 stands at
+ * position ctx_len[q] and node i at ctx_len[q] + node_depth[q][i].  A step is
+ *     spec_draft, spec_tree_metadata,
+ *     the base model's layers over the rows, their attention by spec_tree_attention,
+ *     spec_verify_tree (or spec_penalize and a sampler of the caller's),
+ *     spec_cache_extend with add = n_out, and spec_cache_store of the kept rows' keys and values.
+ * The keys and values of the rows lie beside the cache until it is known which are kept: no cache slot is ever given to a
+ * node that is rejected.  In all of these calls n_nodes[q] = -1 says that sequence q takes no part in the step.  The calls enqueue kernels and
+ * nothing else: they can be recorded into a graph.  They run on the current device, which the pointers must belong to. */
+
+/* Rows of heads: the element (q, r, h, d) is at[q * seq_stride + r * row_stride + h * head_stride + d].  Strides are in
+ * elements, may be negative or zero, and make every row of head_dim elements start on a multiple of 16 bytes. */
+typedef struct {
+  const void* at; /* dev */
+  int64_t seq_stride, row_stride, head_stride;
+} spec_rows_t;
+
+/* A paged cache of keys and values: token t of sequence q lies in block b = block_table[q][t / block_size], slot
+ * t % block_size; its element (h, d) is k[b * block_stride + (t % block_size) * slot_stride + h * head_stride + d], the same
+ * in v.  Strides in elements, rows on multiples of 16 bytes as above. */
+typedef struct {
+  const void* k; /* dev */
+  const void* v; /* dev */
+  int64_t block_stride, slot_stride, head_stride;
+  int32_t n_blocks, block_size; /* n_blocks * block_size <= 2^30 */
+} spec_cache_t;
+
+/* TREE ATTENTION.  For every row r of sequence q and every query head h, with g = h / (q_heads / kv_heads):
+ *     out[q][r][h] = sum_k softmax_k(scale * q[q][r][h] . key_k[g]) value_k[g]
+ * over the ctx_len[q] cached tokens and the rows 0 (the last token), the ancestors of r, and r itself.
+ *   dtype       spec_dtype_t of q, k_new, v_new, cache and out; products and sums in float32
+ *   head_dim    multiple of 8 (SPEC_BF16) or 4 (SPEC_F32), <= 256;  q_heads a multiple of kv_heads
+ *   q, out      rows of q_heads;  k_new, v_new  rows of kv_heads, the same strides for both
+ *   block_table dev [batch, max_blocks] int32;  ctx_len dev [batch] int32, taken as within [0, max_blocks * block_size]
+ *   node_parent dev [batch, M] int32 as spec_tree_metadata writes it (a parent comes before its node; -1: child of
+ *               row 0); may be NULL if M = 0.  A chain of parents is followed over SPEC_MAX_STAGES nodes, the row's own among them
+ *   n_nodes     dev [batch] int32 in [-1, M]; NULL: M everywhere
+ * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.
+ * A cached token whose block is outside [0, n_blocks) takes no part.  Cache slots at and past ctx_len, and rows of k_new and v_new
+ * behind the last node, may hold anything.
+ *   workspace   dev, 16-byte aligned, at least spec_tree_attention_workspace() bytes, contents of no meaning before
+ *               and after; calls that may overlap in time, replays of graphs among them, need one each
+ * Limits: M <= 4096, batch * kv_heads < 2^24, max_blocks * block_size <= 2^30. */
+spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
+                                  const spec_cache_t* cache, const int32_t* block_table, const int32_t* ctx_len,
+                                  const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out, int32_t batch,
+                                  int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                                  int32_t max_blocks, float scale, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream);
+
+/* Bytes of workspace such a call needs (host-only). */
+spec_status_t spec_tree_attention_workspace(int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                            int32_t dtype, int64_t* bytes);
+
+/* BLOCK TABLES AND SLOT MAPS from lengths, on the device: sequence q gets add[q] tokens more (add[q] > 0), or loses its
+ * last -add[q] tokens (add[q] < 0; a finished request: add[q] <= -ctx_len[q]).
+ *   ctx_len     dev [batch]             tokens held so far
+ *   add         dev [batch]
+ *   new_len     dev [batch]             tokens held from now on; may be ctx_len
+ *   added       dev [batch]             new_len - ctx_len: add[q], or 0 where there was no room
+ *   block_table dev [batch, max_blocks] ceil(ctx_len / block_size) entries are in use; entries for the new tokens are written, the
+ *                                       others are left as they were (also those that were given back)
+ *   ring        dev [n_blocks]          free blocks: entries (head + i) % n_blocks, i < count
+ *   ring_state  dev [2]                 head in [0, n_blocks), count in [0, n_blocks]
+ *   ring_state_new dev [2]              the same afterwards; may be ring_state
+ * New blocks come from the ring's head, in batch order; blocks given back go behind its end and are handed out by later calls.  In
+ * batch order, too, requests are served until one does not fit (blocks, or rows of the outputs): it and every growing one
+ * behind it get nothing.  A request that would pass max_blocks is not served and holds up no other.
+ * Where the new tokens go, packed in batch order (cap entries, those behind the last are -1):
+ *   row_start   dev [batch + 1]         first entry of every sequence
+ *   slot        dev [cap]               block * block_size + place in the block
+ *   pos         dev [cap], may be NULL  position in the sequence
+ *   src_row     dev [cap], with path_row only: q * seq_rows + path_row[q][j] for the j-th new token of sequence q
+ *   path_row    dev [batch, path_width], may be NULL: the rows kept by spec_verify_tree
+ * All int32.  Buffers do not overlap, but for new_len and ring_state_new.  n_blocks * block_size, max_blocks * block_size and cap <= 2^30, batch <= 65535. */
+spec_status_t spec_cache_extend(const int32_t* ctx_len, const int32_t* add, int32_t* new_len, int32_t* added, int32_t batch,
+                                int32_t* block_table, int32_t max_blocks, int32_t* ring, int32_t n_blocks,
+                                const int32_t* ring_state, int32_t* ring_state_new, int32_t block_size, int32_t* row_start,
+                                int32_t* slot, int32_t* pos, int32_t* src_row, int32_t cap, const int32_t* path_row,
+                                int32_t path_width, int32_t seq_rows, void* hip_stream);
+
+/* STORE of keys and values into their slots, for `layers` layers of the same shape at once:
+ *     cache[l][slot[t]] = new[l][src_row ? src_row[t] : t]        for t < count, slot[t] in [0, n_blocks * block_size)
+ * Entries with another slot, or a source row outside [0, rows), are skipped.  The slots of one call are distinct.
+ *   k_new, v_new  rows of kv_heads; seq_stride is the distance of two layers
+ *   cache         written; cache_layer_stride is the distance of two of its layers, in elements
+ *   head_dim      as for spec_tree_attention;  slot, src_row dev int32 [count]; src_row may be NULL */
+spec_status_t spec_cache_store(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_cache_t* cache,
+                               int64_t cache_layer_stride, int32_t layers, int32_t rows, int32_t kv_heads, int32_t head_dim,
+                               int32_t dtype, const int32_t* slot, const int32_t* src_row, int32_t count, void* hip_stream);
+
+/* What changes the logits of the rows.  Every pointer (dev) may be NULL; per sequence unless said otherwise.
+ * With W = ceil(vocab / 32) words per row of bits, bit t % 32 of word t / 32 standing for token t:
+ *   counts      [batch, vocab] int32    how often each token was emitted
+ *   seen        [batch, W] uint32       tokens of the prompt or emitted; where given, counts is looked at only where the bit is set
+ *                                       (NULL: seen is counts > 0)
+ *   repetition, presence, frequency     [batch] float32, finite, repetition > 0 (NULL: 1, 0, 0)
+ *   bias        [n_bias, vocab] float32, bias_row [batch] int32: row of the sequence, none where outside [0, n_bias)
+ *   allowed     [n_allowed, W] uint32,   mask_row [batch, R] int32: row of every ROW, none where outside [0, n_allowed) */
+typedef struct {
+  const int32_t* counts;
+  const uint32_t* seen;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const float* bias;
+  const int32_t* bias_row;
+  const uint32_t* allowed;
+  const int32_t* mask_row;
+  int32_t n_bias, n_allowed;
+} spec_penalties_t;
+
+/* PENALTIES, BIASES AND MASKS on the logits of the rows.  With c = counts[t] + the occurrences of t among the nodes on the
+ * row's path (its ancestors and itself), and a token seen if its bit is set or c > 0, in float32, every operation
+ * rounded by itself:
+ *     v = logits[t];   seen: v = v > 0 ? v / repetition : v * repetition;   v = v - frequency * c;
+ *     c > 0: v = v - presence;   v = v + bias[t];   not allowed: v = -inf
+ *   logits, out [batch, R, vocab] logits_dtype; out may be logits.  Rows behind the last node are left as they were
+ *   node_tok, node_parent [batch, M], n_nodes [batch]: as for spec_tree_attention; node_tok, node_parent may be NULL
+ *   (no path counts), n_nodes NULL: M everywhere
+ *   pen  host */
+spec_status_t spec_penalize(const void* logits, int32_t logits_dtype, int32_t batch, int32_t M, int32_t vocab,
+                            const spec_penalties_t* pen, const int32_t* node_tok, const int32_t* node_parent,
+                            const int32_t* n_nodes, void* out, void* hip_stream);
+
+/* VERIFY on the rows of the tree, greedy (spec_verify on logits that hold every shared prefix once), with the
+ * penalties applied on the fly.
+ *   logits      dev [batch, R, vocab] logits_dtype;  pen host, may be NULL
+ *   cand_tokens, cand_node dev [batch, B, n_predict] as spec_draft and spec_tree_metadata write them (n_predict = 0: NULL)
+ *   n_cand      dev [batch], may be NULL: sequence q has candidates [0, n_cand[q]) only
+ * Outputs (dev, int32):
+ *   greedy      [batch, R]               first maximum of the processed row (0 where nothing is above -inf); -1 behind the last node
+ *   accept_len, best_cand, n_out [batch], out_tokens [batch, n_predict + 1], accept_all [batch, B] (may be NULL): as spec_verify;
+ *                                        all 0, out_tokens -1, for a sequence that takes no part
+ *   path_row    [batch, n_predict + 1]   rows of the kept tokens: 0, then the accepted nodes', then -1: the next hidden state
+ *                                        is row path_row[accept_len]'s
+ *   counts_out, seen_out                 may be NULL; where given (pen's counts and seen, without const), the emitted tokens are
+ *                                        added to them
+ * A node whose row is not among the sequence's rows is never accepted.  M <= 4096, 0 <= n_predict <= SPEC_MAX_STAGES. */
+spec_status_t spec_verify_tree(const void* logits, int32_t logits_dtype, const int32_t* cand_tokens, const int32_t* cand_node,
+                               const int32_t* n_cand, const int32_t* node_tok, const int32_t* node_parent,
+                               const int32_t* n_nodes, const spec_penalties_t* pen, int32_t batch, int32_t M, int32_t B,
+                               int32_t n_predict, int32_t vocab, int32_t* greedy, int32_t* accept_len, int32_t* best_cand,
+                               int32_t* out_tokens, int32_t* n_out, int32_t* path_row, int32_t* accept_all,
+                               int32_t* counts_out, uint32_t* seen_out, void* hip_stream);
+
 /* Measurement aid, not a step of the method: one launch of a plain copy kernel that
  * reads `bytes` from src (dev) and writes them to dst (dev; must not overlap src).  Its HBM
  * traffic is known exactly, which calibrates the memory-traffic hardware counters that

@@ -22,7 +22,8 @@ SPEC_OK, SPEC_EINVAL, SPEC_ESHAPE, SPEC_EDTYPE, SPEC_ENOMEM, SPEC_EHIP = 0, -1, 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecdraft.so")
 
 EXPORTS = ["spec_create", "spec_destroy", "spec_draft", "spec_draft_static", "spec_draft_dynamic", "spec_verify", "spec_verify_dynamic", "spec_head_logp", "spec_model_scalars",
-           "spec_profile_enable", "spec_profile_read", "spec_copy_probe", "spec_tree_metadata", "spec_advance", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
+           "spec_profile_enable", "spec_profile_read", "spec_copy_probe", "spec_tree_metadata", "spec_advance", "spec_tree_attention", "spec_tree_attention_workspace", "spec_cache_extend",
+           "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
 
 
 class SpecError(RuntimeError):
@@ -45,6 +46,20 @@ class spec_weights_t(C.Structure):
 class spec_plan_t(C.Structure):
     _fields_ = [(name, C.c_int32) for name in ("kernel", "block_rows", "tile_rows", "row_blocks", "ranges", "tiles",
                                                "parts", "k_split", "workgroups", "lds_bytes", "proj_apart")]
+
+
+class spec_rows_t(C.Structure):
+    _fields_ = [("at", C.c_void_p), ("seq_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class spec_cache_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("block_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("n_blocks", C.c_int32), ("block_size", C.c_int32)]
+
+
+class spec_penalties_t(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("counts", "seen", "repetition", "presence", "frequency", "bias", "bias_row",
+                                                "allowed", "mask_row")] + [("n_bias", C.c_int32), ("n_allowed", C.c_int32)]
 
 
 class spec_debug_t(C.Structure):
@@ -108,6 +123,21 @@ def lib() -> C.CDLL:
         l.spec_tree_metadata.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 7
         l.spec_advance.restype = C.c_int
         l.spec_advance.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 6
+        rows, cache, pen, i32, ptr = C.POINTER(spec_rows_t), C.POINTER(spec_cache_t), C.POINTER(spec_penalties_t), C.c_int32, C.c_void_p
+        l.spec_tree_attention.restype = C.c_int
+        l.spec_tree_attention.argtypes = ([rows] * 3 + [cache] + [ptr] * 4 + [rows] + [i32] * 7
+                                          + [C.c_float, ptr, C.c_int64, ptr])
+        l.spec_tree_attention_workspace.restype = C.c_int
+        l.spec_tree_attention_workspace.argtypes = [i32] * 6 + [C.POINTER(C.c_int64)]
+        l.spec_cache_extend.restype = C.c_int
+        l.spec_cache_extend.argtypes = ([ptr] * 4 + [i32, ptr, i32, ptr, i32, ptr, ptr, i32] + [ptr] * 4
+                                        + [i32, ptr, i32, i32, ptr])
+        l.spec_cache_store.restype = C.c_int
+        l.spec_cache_store.argtypes = [rows, rows, cache, C.c_int64] + [i32] * 5 + [ptr, ptr, i32, ptr]
+        l.spec_penalize.restype = C.c_int
+        l.spec_penalize.argtypes = [ptr] + [i32] * 4 + [pen] + [ptr] * 5
+        l.spec_verify_tree.restype = C.c_int
+        l.spec_verify_tree.argtypes = [ptr, i32] + [ptr] * 6 + [pen] + [i32] * 5 + [ptr] * 10
         l.spec_copy_probe.restype = C.c_int
         l.spec_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         l.spec_last_error.restype = C.c_char_p
@@ -506,6 +536,268 @@ def spec_advance(hidden: torch.Tensor, best_cand: torch.Tensor, accept_len: torc
     _require(next_tok, "next_tok", torch.int32, (b,))
     _check(lib().spec_advance(_ptr(hidden), dtype, b, Bc, n1 - 1, E, _ptr(best_cand), _ptr(accept_len),
                               _ptr(out_tokens), _ptr(next_state), _ptr(next_tok), _stream_ptr(stream)))
+
+
+# ---- around the base model's forward over the token tree: rows of every sequence = the last token, then the tree's nodes ----
+
+def _here(stream, **tensors) -> None:
+    """Every tensor that is given lies on the current device, and so does the stream: the kernels run there."""
+    if not _CHECK_DEVICE:
+        return
+    at = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        at = torch.cuda.current_device() if at is None else at
+        if t.get_device() != at:
+            raise ValueError("%s lies on device %d, the current device is %d" % (name, t.get_device(), at))
+    on = getattr(stream, "device", None)
+    if on is not None and on.index is not None and at is not None and on.index != at:
+        raise ValueError("the stream belongs to device %d, the current device is %d" % (on.index, at))
+
+
+def _float_code(t, name: str, dims: Sequence[int]) -> int:
+    if not isinstance(t, torch.Tensor) or t.dim() not in dims:
+        raise ValueError("%s must be a tensor of %s dimensions" % (name, " or ".join(str(d) for d in dims)))
+    code = _DTYPE_CODE.get(t.dtype, -1)
+    if code < 0:
+        raise ValueError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return code
+
+
+def _strided(t, name: str, dtype: torch.dtype, shape: Sequence[int]) -> List[int]:
+    """Strides of a tensor whose last dimension is contiguous (0 along dimensions of one entry, whose stride says nothing)."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s must be a torch.Tensor" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+
+
+def _written(t, name: str) -> None:
+    """A tensor that is written through strides must not hold an element twice."""
+    if any(n > 1 and t.stride(i) == 0 for i, n in enumerate(t.shape)):
+        raise ValueError("%s is written and must not be expanded" % name)
+
+
+def spec_tree_attention_workspace(batch: int, R: int, q_heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace of spec_tree_attention with R rows per sequence (host-only: needs no GPU)."""
+    code = _DTYPE_CODE.get(dtype, -1)
+    out = C.c_int64()
+    _check(lib().spec_tree_attention_workspace(int(batch), int(R) - 1, int(q_heads), int(kv_heads), int(head_dim), code, C.byref(out)))
+    return int(out.value)
+
+
+def spec_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.Tensor,
+                        v_cache: torch.Tensor, block_table: torch.Tensor, ctx_len: torch.Tensor,
+                        node_parent: Optional[torch.Tensor], n_nodes: Optional[torch.Tensor], out: torch.Tensor,
+                        workspace: torch.Tensor, scale: Optional[float] = None, stream=None) -> None:
+    """Enqueues the attention of R = M + 1 rows per sequence over the cache and their own ancestors.
+
+    q, out [batch, R, q_heads, head_dim]; k_new, v_new [batch, R, kv_heads, head_dim]; k_cache, v_cache [n_blocks, block_size,
+    kv_heads, head_dim]: any strides but along head_dim, rows on 16 bytes, the same strides in k_* and v_*.  node_parent [batch, M]
+    (None: M = 0), n_nodes [batch] (None: M each).  workspace: contiguous uint8, spec_tree_attention_workspace() bytes, not
+    shared by calls that may overlap in time.  scale: head_dim ** -0.5 by default."""
+    code = _float_code(q, "q", (4,))
+    b, R, H, D = q.shape
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a [n_blocks, block_size, kv_heads, head_dim] tensor")
+    if R < 1:
+        raise ValueError("q needs a row per sequence")
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [batch, max_blocks] tensor")
+    n_blocks, page, KH, _ = k_cache.shape
+    sq, so = _strided(q, "q", q.dtype, (b, R, H, D)), _strided(out, "out", q.dtype, (b, R, H, D))
+    sk, sv = _strided(k_new, "k_new", q.dtype, (b, R, KH, D)), _strided(v_new, "v_new", q.dtype, (b, R, KH, D))
+    ck = _strided(k_cache, "k_cache", q.dtype, (n_blocks, page, KH, D))
+    cv = _strided(v_cache, "v_cache", q.dtype, (n_blocks, page, KH, D))
+    if ck != cv or sk != sv:
+        raise ValueError("k_cache and v_cache, and k_new and v_new, must have the same strides")
+    _written(out, "out")
+    M, width = R - 1, int(block_table.shape[1])
+    _require(block_table, "block_table", torch.int32, (b, width))
+    _require(ctx_len, "ctx_len", torch.int32, (b,))
+    _require(node_parent, "node_parent", torch.int32, (b, M), optional=M == 0)
+    _require(n_nodes, "n_nodes", torch.int32, (b,), optional=True)
+    _require(workspace, "workspace", torch.uint8)
+    _here(stream, q=q, out=out, k_new=k_new, v_new=v_new, k_cache=k_cache, v_cache=v_cache, block_table=block_table, ctx_len=ctx_len,
+          node_parent=node_parent, n_nodes=n_nodes, workspace=workspace)
+    cache = spec_cache_t(_ptr(k_cache), _ptr(v_cache), *ck, n_blocks, page)
+    _check(lib().spec_tree_attention(
+        C.byref(spec_rows_t(_ptr(q), *sq)), C.byref(spec_rows_t(_ptr(k_new), *sk)), C.byref(spec_rows_t(_ptr(v_new), *sv)),
+        C.byref(cache), _ptr(block_table), _ptr(ctx_len), _ptr(node_parent), _ptr(n_nodes), C.byref(spec_rows_t(_ptr(out), *so)),
+        b, M, H, KH, D, code, width, D ** -0.5 if scale is None else float(scale), _ptr(workspace) or None, workspace.numel(),
+        _stream_ptr(stream)))
+
+
+def spec_cache_extend(ctx_len: torch.Tensor, add: torch.Tensor, new_len: torch.Tensor, added: torch.Tensor,
+                      block_table: torch.Tensor, ring: torch.Tensor, ring_state: torch.Tensor, ring_state_new: torch.Tensor,
+                      block_size: int, row_start: torch.Tensor, slot: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                      path_row: Optional[torch.Tensor] = None, seq_rows: int = 0, src_row: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """Enqueues the block tables and slot maps for add[q] tokens more (or fewer) per sequence.
+
+    ctx_len, add, new_len, added [batch]; block_table [batch, max_blocks]; ring [n_blocks]; ring_state, ring_state_new [2];
+    row_start [batch + 1]; slot, pos, src_row [cap]; path_row [batch, path_width] with src_row: all int32.  new_len may be
+    ctx_len and ring_state_new may be ring_state; no other two may share memory."""
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or not isinstance(ring, torch.Tensor) or ring.dim() != 1:
+        raise ValueError("block_table must be a [batch, max_blocks] tensor and ring a [n_blocks] tensor")
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
+        raise ValueError("slot must be a [cap] tensor")
+    (b, width), cap, i32 = block_table.shape, int(slot.shape[0]), torch.int32
+    _require(block_table, "block_table", i32)
+    for t, name in ((ctx_len, "ctx_len"), (add, "add"), (new_len, "new_len"), (added, "added")):
+        _require(t, name, i32, (b,))
+    _require(ring, "ring", i32)
+    _require(ring_state, "ring_state", i32, (2,))
+    _require(ring_state_new, "ring_state_new", i32, (2,))
+    _require(row_start, "row_start", i32, (b + 1,))
+    _require(slot, "slot", i32)
+    _require(pos, "pos", i32, (cap,), optional=True)
+    path_width = 0
+    if path_row is not None:
+        if not isinstance(path_row, torch.Tensor) or path_row.dim() != 2:
+            raise ValueError("path_row must be a [batch, path_width] tensor")
+        path_width = int(path_row.shape[1])
+        _require(path_row, "path_row", i32, (b, path_width))
+        _require(src_row, "src_row", i32, (cap,))
+    elif src_row is not None:
+        raise ValueError("src_row is written with path_row only")
+    _here(stream, ctx_len=ctx_len, add=add, new_len=new_len, added=added, block_table=block_table, ring=ring, ring_state=ring_state,
+          ring_state_new=ring_state_new, row_start=row_start, slot=slot, pos=pos, path_row=path_row, src_row=src_row)
+    _check(lib().spec_cache_extend(_ptr(ctx_len), _ptr(add), _ptr(new_len), _ptr(added), b, _ptr(block_table), width, _ptr(ring),
+                                   int(ring.shape[0]), _ptr(ring_state), _ptr(ring_state_new), int(block_size), _ptr(row_start),
+                                   _ptr(slot), _ptr(pos), _ptr(src_row), cap, _ptr(path_row), path_width, int(seq_rows),
+                                   _stream_ptr(stream)))
+
+
+def spec_cache_store(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                     src_row: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueues the copy of rows into their cache slots: row src_row[t] (or t) to slot[t], entries without a slot skipped.
+
+    One layer: k_new, v_new [rows, kv_heads, head_dim], k_cache, v_cache [n_blocks, block_size, kv_heads, head_dim].  Several at
+    once: a first dimension of layers in all four.  Strides as for spec_tree_attention; slot, src_row [count] int32."""
+    code = _float_code(k_cache, "k_cache", (4, 5))
+    if not isinstance(k_new, torch.Tensor) or not isinstance(v_new, torch.Tensor) or not isinstance(v_cache, torch.Tensor):
+        raise ValueError("k_new, v_new and v_cache must be tensors")
+    if k_cache.dim() == 4 and k_new.dim() == 3 and v_new.dim() == 3 and v_cache.dim() == 4:
+        k_new, v_new, k_cache, v_cache = (t.unsqueeze(0) for t in (k_new, v_new, k_cache, v_cache))
+    if k_new.dim() != 4 or k_cache.dim() != 5:
+        raise ValueError("k_new must have one dimension less than k_cache")
+    L, n_blocks, page, KH, D = k_cache.shape
+    rows = int(k_new.shape[1])
+    sk, sv = _strided(k_new, "k_new", k_cache.dtype, (L, rows, KH, D)), _strided(v_new, "v_new", k_cache.dtype, (L, rows, KH, D))
+    ck = _strided(k_cache, "k_cache", k_cache.dtype, (L, n_blocks, page, KH, D))
+    cv = _strided(v_cache, "v_cache", k_cache.dtype, (L, n_blocks, page, KH, D))
+    if ck != cv or sk != sv:
+        raise ValueError("k_cache and v_cache, and k_new and v_new, must have the same strides")
+    _written(k_cache, "k_cache")
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
+        raise ValueError("slot must be a [count] tensor")
+    count = int(slot.shape[0])
+    _require(slot, "slot", torch.int32, (count,))
+    _require(src_row, "src_row", torch.int32, (count,), optional=True)
+    _here(stream, k_new=k_new, v_new=v_new, k_cache=k_cache, v_cache=v_cache, slot=slot, src_row=src_row)
+    _check(lib().spec_cache_store(C.byref(spec_rows_t(_ptr(k_new), *sk)), C.byref(spec_rows_t(_ptr(v_new), *sv)),
+                                  C.byref(spec_cache_t(_ptr(k_cache), _ptr(v_cache), *ck[1:], n_blocks, page)), ck[0], L, rows, KH, D,
+                                  code, _ptr(slot), _ptr(src_row), count, _stream_ptr(stream)))
+
+
+_PENALTIES = ("counts", "seen", "repetition", "presence", "frequency", "bias", "bias_row", "allowed", "mask_row")
+
+
+def _penalties(pen: Dict[str, torch.Tensor], b: int, R: int, V: int, stream) -> spec_penalties_t:
+    for key in pen:
+        if key not in _PENALTIES:
+            raise ValueError("penalties[%s]: not one of %s" % (key, ", ".join(_PENALTIES)))
+    t = {k: pen.get(k) for k in _PENALTIES}
+    words, i32, f32 = (V + 31) // 32, torch.int32, torch.float32
+    n_bias, n_allowed = (int(t[k].shape[0]) if isinstance(t[k], torch.Tensor) and t[k].dim() == 2 else 0 for k in ("bias", "allowed"))
+    for name, dt, shape in (("counts", i32, (b, V)), ("seen", i32, (b, words)), ("repetition", f32, (b,)), ("presence", f32, (b,)),
+                            ("frequency", f32, (b,)), ("bias", f32, (n_bias, V)), ("bias_row", i32, (b,)),
+                            ("allowed", i32, (n_allowed, words)), ("mask_row", i32, (b, R))):
+        _require(t[name], "penalties[%s]" % name, dt, shape, optional=True)
+    if (t["bias"] is None) != (t["bias_row"] is None) or (t["allowed"] is None) != (t["mask_row"] is None):
+        raise ValueError("bias goes with bias_row, and allowed with mask_row")
+    _here(stream, **{"penalties[%s]" % k: v for k, v in t.items()})
+    return spec_penalties_t(*[_ptr(t[k]) or None for k in _PENALTIES], n_bias, n_allowed)
+
+
+def spec_penalize(logits: torch.Tensor, out: torch.Tensor, penalties: Dict[str, torch.Tensor],
+                  node_tok: Optional[torch.Tensor] = None, node_parent: Optional[torch.Tensor] = None,
+                  n_nodes: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueues penalties, biases and masks on logits [batch, R, vocab] into out (which may be logits).
+
+    penalties: any of counts [batch, vocab] int32, seen [batch, W] int32, repetition / presence / frequency [batch] float32,
+    bias [n_bias, vocab] float32 with bias_row [batch] int32, allowed [n_allowed, W] int32 with mask_row [batch, R] int32, where
+    W = ceil(vocab / 32) words of 32 bits, the lowest first.  node_tok, node_parent [batch, R - 1]: rows count the tokens on their path."""
+    code = _float_code(logits, "logits", (3,))
+    b, R, V = logits.shape
+    if R < 1:
+        raise ValueError("logits need a row per sequence")
+    _require(logits, "logits", logits.dtype)
+    _require(out, "out", logits.dtype, (b, R, V))
+    _require(node_tok, "node_tok", torch.int32, (b, R - 1), optional=True)
+    _require(node_parent, "node_parent", torch.int32, (b, R - 1), optional=True)
+    _require(n_nodes, "n_nodes", torch.int32, (b,), optional=True)
+    if (node_tok is None) != (node_parent is None):
+        raise ValueError("node_tok and node_parent go together")
+    pen = _penalties(penalties, b, R, V, stream)
+    _here(stream, logits=logits, out=out, node_tok=node_tok, node_parent=node_parent, n_nodes=n_nodes)
+    _check(lib().spec_penalize(_ptr(logits), code, b, R - 1, V, C.byref(pen), _ptr(node_tok) or None, _ptr(node_parent) or None,
+                               _ptr(n_nodes), _ptr(out), _stream_ptr(stream)))
+
+
+def spec_verify_tree(logits: torch.Tensor, cand_tokens: torch.Tensor, cand_node: torch.Tensor, n_nodes: Optional[torch.Tensor],
+                     greedy: torch.Tensor, accept_len: torch.Tensor, best_cand: torch.Tensor, out_tokens: torch.Tensor,
+                     n_out: torch.Tensor, path_row: torch.Tensor, accept_all: Optional[torch.Tensor] = None,
+                     n_cand: Optional[torch.Tensor] = None, penalties: Optional[Dict[str, torch.Tensor]] = None,
+                     node_tok: Optional[torch.Tensor] = None, node_parent: Optional[torch.Tensor] = None, update: bool = False,
+                     stream=None) -> None:
+    """Enqueues one verify on logits [batch, R, vocab] of the tree's rows, with penalties as spec_penalize applies them.
+
+    cand_tokens, cand_node [batch, B, n] (n = 0 and B = 1: plain decoding); greedy [batch, R]; accept_len, best_cand, n_out
+    [batch]; out_tokens, path_row [batch, n + 1]; accept_all [batch, B].  update: the emitted tokens are added to
+    penalties' counts and seen."""
+    code = _float_code(logits, "logits", (3,))
+    b, R, V = logits.shape
+    if R < 1:
+        raise ValueError("logits need a row per sequence")
+    if not isinstance(cand_tokens, torch.Tensor) or cand_tokens.dim() != 3:
+        raise ValueError("cand_tokens must be a [batch, B, n_predict] tensor")
+    i32, (_, Bc, n) = torch.int32, cand_tokens.shape
+    _require(logits, "logits", logits.dtype)
+    _require(cand_tokens, "cand_tokens", i32, (b, Bc, n))
+    _require(cand_node, "cand_node", i32, (b, Bc, n))
+    _require(greedy, "greedy", i32, (b, R))
+    for t, name in ((accept_len, "accept_len"), (best_cand, "best_cand"), (n_out, "n_out")):
+        _require(t, name, i32, (b,))
+    _require(out_tokens, "out_tokens", i32, (b, n + 1))
+    _require(path_row, "path_row", i32, (b, n + 1))
+    _require(accept_all, "accept_all", i32, (b, Bc), optional=True)
+    for t, name in ((n_cand, "n_cand"), (n_nodes, "n_nodes")):
+        _require(t, name, i32, (b,), optional=True)
+    for t, name in ((node_tok, "node_tok"), (node_parent, "node_parent")):
+        _require(t, name, i32, (b, R - 1), optional=True)
+    if (node_tok is None) != (node_parent is None):
+        raise ValueError("node_tok and node_parent go together")
+    pen = None if penalties is None else _penalties(penalties, b, R, V, stream)
+    if update and pen is None:
+        raise ValueError("update needs penalties")
+    _here(stream, logits=logits, cand_tokens=cand_tokens, cand_node=cand_node, n_nodes=n_nodes, greedy=greedy, accept_len=accept_len,
+          best_cand=best_cand, out_tokens=out_tokens, n_out=n_out, path_row=path_row, accept_all=accept_all, n_cand=n_cand,
+          node_tok=node_tok, node_parent=node_parent)
+    _check(lib().spec_verify_tree(
+        _ptr(logits), code, _ptr(cand_tokens) or None, _ptr(cand_node) or None, _ptr(n_cand), _ptr(node_tok) or None,
+        _ptr(node_parent) or None, _ptr(n_nodes), C.byref(pen) if pen is not None else None, b, R - 1, Bc, n, V, _ptr(greedy),
+        _ptr(accept_len), _ptr(best_cand), _ptr(out_tokens), _ptr(n_out), _ptr(path_row), _ptr(accept_all),
+        pen.counts if update else None, pen.seen if update else None, _stream_ptr(stream)))
 
 
 def spec_plan_contraction(rows: int, k: int, n_head: int, k_top: int, n_proj: int, n_cu: int = 256) -> dict:

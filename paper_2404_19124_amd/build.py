@@ -33,6 +33,10 @@ SOURCES = [
     "kernels_head_panel.hip",
     "kernels_head_once.hip",
     "kernels_tree_meta.hip",
+    "kernels_tree_attention.hip",
+    "kernels_cache.hip",
+    "kernels_rows.hip",
+    "rows_lib.hip",
 ]
 
 FLAGS = [

@@ -1,0 +1,172 @@
+// The cache that spec_tree_attention reads: which blocks a sequence holds, where its next tokens go, and the copy of
+// their keys and values into those slots.
+#include "device_utils.h"
+#include "rows_internal.h"
+#include "spec_internal.h"
+
+namespace specdraft {
+
+// sums of 65535 demands of up to 2^30 tokens
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint64_t y = __shfl_up((unsigned long long)x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// blocks that `len` tokens need
+__device__ __forceinline__ int blocks_of(int len, int size) { return (int)(((uint32_t)len + (uint32_t)size - 1) / (uint32_t)size); }
+
+// One workgroup: prefix sums over the batch of the blocks and rows that are asked for.  A sequence is served while both sums
+// fit, so the served ones come before the first that is not, and a sequence's share starts where the sum before it ends.
+__global__ __launch_bounds__(1024) void extend_plan_kernel(ExtendJob p) {
+  __shared__ uint64_t part[3][16];
+  __shared__ unsigned long long s_fit[2];   // blocks and rows of the served ones: the sums in front of the first that is not
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int head = min(max(p.ring_state[0], 0), p.n_blocks - 1), count = min(max(p.ring_state[1], 0), p.n_blocks);
+  const int limit = p.max_blocks * p.block_size;
+  if (tid < 2) s_fit[tid] = ~0ull;
+  uint64_t carry[3] = {0, 0, 0};
+  for (int q0 = 0; q0 < p.batch; q0 += 1024) {
+    const int q = q0 + tid;
+    uint64_t x[3] = {0, 0, 0};   // blocks and rows asked for, blocks given back
+    int old = 0, a = 0;
+    if (q < p.batch) {
+      old = min(max(p.ctx_len[q], 0), limit);
+      a = p.add[q];
+      if (a > limit - old) a = 0;
+      if (a < -old) a = -old;
+      const int have = blocks_of(old, p.block_size), want = blocks_of(old + a, p.block_size);
+      if (a > 0) x[0] = want - have, x[1] = a;
+      else x[2] = have - want;
+    }
+    uint64_t sum[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sum[i] = wave_scan(x[i]);
+    __syncthreads();   // the last round's sums have been read; s_fit is set
+    if (lane == 63)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) part[i][wave] = sum[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      uint64_t before = carry[i];
+      for (int w = 0; w < 16; ++w) {
+        if (w < wave) before += part[i][w];
+        carry[i] += part[i][w];
+      }
+      sum[i] += before;
+    }
+    const bool served = a <= 0 || (sum[0] <= (uint64_t)count && sum[1] <= (uint64_t)p.cap);
+    if (!served) {
+      atomicMin(&s_fit[0], (unsigned long long)(sum[0] - x[0]));
+      atomicMin(&s_fit[1], (unsigned long long)(sum[1] - x[1]));
+    }
+    __syncthreads();
+    if (q < p.batch) {
+      p.new_len[q] = served ? old + a : old;
+      p.added[q] = served ? a : 0;
+      p.row_start[q] = (int32_t)min((uint64_t)s_fit[1], sum[1] - x[1]);
+    }
+  }
+  if (tid == 0) {
+    const uint64_t taken = min((uint64_t)s_fit[0], carry[0]);
+    p.row_start[p.batch] = (int32_t)min((uint64_t)s_fit[1], carry[1]);
+    p.ring_state_new[0] = (int32_t)(((uint64_t)head + taken) % (uint64_t)p.n_blocks);
+    p.ring_state_new[1] = (int32_t)min((uint64_t)count - taken + carry[2], (uint64_t)p.n_blocks);
+  }
+}
+
+// Workgroup (q, y) carries out sequence q's share, strided over y; the ones behind the last sequence mark the entries behind
+// the last token.  Where a share starts in the ring is summed up once more from the lengths: a few words from the cache, and
+// no workspace.  Reads and writes of the ring do not meet: what is taken lies among its `count` entries, what is given
+// back goes behind them.
+__global__ __launch_bounds__(256) void extend_fill_kernel(ExtendJob p) {
+  __shared__ uint64_t part[4][4];
+  const int q = blockIdx.x, tid = threadIdx.x, at = blockIdx.y * 256 + tid, step = gridDim.y * 256;
+  if (q == p.batch) {
+    for (int t = p.row_start[p.batch] + at; t < p.cap; t += step) {
+      p.slot[t] = -1;
+      if (p.pos) p.pos[t] = -1;
+      if (p.path_row) p.src_row[t] = -1;
+    }
+    return;
+  }
+  const int a = p.added[q];
+  if (a == 0) return;
+  uint64_t sum[4] = {0, 0, 0, 0};   // blocks taken and given back: before this sequence, by all
+  for (int i = tid; i < p.batch; i += 256) {
+    const int d = p.added[i], now = p.new_len[i];
+    const int change = blocks_of(now, p.block_size) - blocks_of(now - d, p.block_size);
+    sum[2] += max(change, 0);
+    sum[3] += max(-change, 0);
+    if (i < q) sum[0] += max(change, 0), sum[1] += max(-change, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sum[i] = wave_scan(sum[i]);
+    if ((tid & 63) == 63) part[i][tid >> 6] = sum[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = part[i][0] + part[i][1] + part[i][2] + part[i][3];
+  const uint64_t n = p.n_blocks;
+  // (the ring before this call)
+  const uint64_t head = ((uint64_t)p.ring_state_new[0] + n - sum[2] % n) % n;
+  const uint64_t count = (uint64_t)p.ring_state_new[1] + sum[2] - sum[3];
+  const int now = p.new_len[q], old = now - a;
+  const int have = blocks_of(old, p.block_size), want = blocks_of(now, p.block_size);
+  int32_t* row = p.block_table + (int64_t)q * p.max_blocks;
+  if (a < 0) {
+    for (int i = want + at; i < have; i += step) p.ring[(head + count + sum[1] + (uint64_t)(i - want)) % n] = row[i];
+    return;
+  }
+  for (int i = have + at; i < want; i += step) row[i] = p.ring[(head + sum[0] + (uint64_t)(i - have)) % n];
+  const int first = p.row_start[q];
+  for (int j = at; j < a; j += step) {
+    const int t = old + j, b = t / p.block_size;
+    // (a new block's entry may be under way to the table)
+    const int block = b < have ? row[b] : p.ring[(head + sum[0] + (uint64_t)(b - have)) % n];
+    p.slot[first + j] = block >= 0 && block < p.n_blocks ? block * p.block_size + t % p.block_size : -1;
+    if (p.pos) p.pos[first + j] = t;
+    if (p.path_row) {
+      const int r = j < p.path_width ? p.path_row[(int64_t)q * p.path_width + j] : -1;
+      p.src_row[first + j] = r >= 0 && r < p.seq_rows ? q * p.seq_rows + r : -1;
+    }
+  }
+}
+
+hipError_t launch_extend(const ExtendJob& job, hipStream_t st) {
+  hipLaunchKernelGGL(extend_plan_kernel, dim3(1), dim3(1024), 0, st, job);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int most = job.cap / 1024 + 1;
+  hipLaunchKernelGGL(extend_fill_kernel, dim3(job.batch + 1, most < 32 ? most : 32), dim3(256), 0, st, job);
+  return hipGetLastError();
+}
+
+// Copy of one 16-byte word of a token's keys and one of its values per thread and turn.
+__global__ __launch_bounds__(256) void store_kernel(StoreJob p) {
+  const int per = p.kv_heads * p.row_words, layer = blockIdx.y;
+  const int64_t total = (int64_t)p.count * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int t = (int)(i / per), w = (int)(i - (int64_t)t * per), h = w / p.row_words, c = w - h * p.row_words;
+    const int slot = p.slot[t], src = p.src_row ? p.src_row[t] : t;
+    if (slot < 0 || slot >= p.n_slots || src < 0 || src >= p.rows) continue;
+    const int64_t from = layer * p.new_layer + src * p.new_row + h * p.new_head + c * 16;
+    const int64_t to = layer * p.layer + slot / p.block_size * p.block + slot % p.block_size * p.slot_stride + h * p.head + c * 16;
+    *reinterpret_cast<u32x4*>(p.k + to) = *reinterpret_cast<const u32x4*>(p.k_new + from);
+    *reinterpret_cast<u32x4*>(p.v + to) = *reinterpret_cast<const u32x4*>(p.v_new + from);
+  }
+}
+
+hipError_t launch_store(const StoreJob& job, hipStream_t st) {
+  const int64_t words = (int64_t)job.count * job.kv_heads * job.row_words, groups = (words + 255) / 256;
+  hipLaunchKernelGGL(store_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096), job.layers), dim3(256), 0, st, job);
+  return hipGetLastError();
+}
+
+}  // namespace specdraft

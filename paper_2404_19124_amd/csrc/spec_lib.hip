@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "spec_internal.h"
+#include "status.h"
 #include "tickets.h"
 
 using namespace specdraft;
@@ -25,21 +26,16 @@ static_assert(SPEC_MAX_LEAVES == kMaxLeaves, "header and kernels disagree");
 
 static thread_local char g_err[512] = "";
 
-static spec_status_t fail(spec_status_t code, const char* fmt, ...) {
+spec_status_t specdraft::fail(spec_status_t code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
-static spec_status_t hip_fail(hipError_t e, const char* what) {
+spec_status_t specdraft::hip_fail(hipError_t e, const char* what) {
   return fail(SPEC_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
-#define HIP_TRY(expr)                                  \
-  do {                                                 \
-    hipError_t e_ = (expr);                            \
-    if (e_ != hipSuccess) return hip_fail(e_, #expr);  \
-  } while (0)
 
 // Device memory a draft uses beyond its inputs and outputs.  Every buffer is written before it
 // is read within one call; nothing has to start at zero.
