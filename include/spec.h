@@ -324,7 +324,7 @@ typedef struct {
  * behind the last node, may hold anything.
  *   workspace   dev, 16-byte aligned, at least spec_tree_attention_workspace() bytes, contents of no meaning before
  *               and after; calls that may overlap in time, replays of graphs among them, need one each
- * Limits: M <= 4096, batch * kv_heads < 2^24, max_blocks * block_size <= 2^30. */
+ * Limits: M <= 4096, batch and q_heads <= 65535, max_blocks * block_size <= 2^30. */
 spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
                                   const spec_cache_t* cache, const int32_t* block_table, const int32_t* ctx_len,
                                   const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out, int32_t batch,

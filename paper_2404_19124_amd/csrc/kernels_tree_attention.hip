@@ -17,7 +17,10 @@ namespace specdraft {
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -39,16 +42,24 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// values that are the same in every lane, in scalar registers
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
 // A sequence's share of the tiles.
 struct SeqTiles {
   int ctx, nodes, tiles, blocks;   // cached tokens, last row, tiles per unit, units per key/value head
   uint64_t total;                  // tiles of all units
 };
-template <int KT>
+template <int KT, bool UNIFORM = false>
 __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int BM) {
   SeqTiles s;
-  s.ctx = min(max(p.ctx_len[q], 0), p.max_blocks * p.block_size);
-  s.nodes = p.n_nodes ? min(max(p.n_nodes[q], -1), p.M) : p.M;
+  int ctx = p.ctx_len[q], nodes = p.n_nodes ? p.n_nodes[q] : p.M;
+  if (UNIFORM) ctx = uniform(ctx), nodes = uniform(nodes);
+  s.ctx = min(max(ctx, 0), p.max_blocks * p.block_size);
+  s.nodes = min(max(nodes, -1), p.M);
   s.tiles = (s.ctx + s.nodes + KT) / KT;
   s.blocks = (int)(((int64_t)(s.nodes + 1) * (p.q_heads / p.kv_heads) + BM - 1) / BM);
   s.total = (uint64_t)s.tiles * (uint64_t)s.blocks * (uint64_t)p.kv_heads;
@@ -83,14 +94,249 @@ struct AttentionShape {
   static_assert((WK - 1) * WQ * 64 * MQ * (DP / 4 + 2) * 4 <= LDS, "the waves' results fit the tiles' memory");
 };
 
+// One tile of one unit: scores, softmax and values of a wave's keys and query rows.
+template <bool BF16, int DP, int MQ, int WK, int KT>
+struct AttentionTile {
+  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
+  typedef typename std::conditional<BF16, bf16x8, f32x4>::type qword;
+  static constexpr int QS = BF16 ? DP / 32 : DP / 16;   // steps along the head
+  qword qf[MQ][QS];       // queries: lane l16 of every group holds row l16 of each block of 16
+  int row_of[MQ];         // tree rows of this lane's query rows
+  f32x4 o[MQ][DP / 16];   // transposed: elements 16 d + 4 grp + i of the head, query row l16
+  float m_run[MQ], l_run[MQ];
+
+  // `sees_cached`: which of the tile's keys are cached tokens; t0: its first key
+  __device__ __forceinline__ void step(const lds_u8* kb, const lds_u8* vb, uint64_t cached, int t0, int ctx, const uint16_t* s_up, float sc) {
+    constexpr int ROWB = S::ROWB, KW = S::KW, NB = S::NB, SWZ = S::SWZ;
+    const int tid = opaque_tid(), lane = tid & 63, l16 = lane & 15, grp = lane >> 4, wk = (tid >> 6) % WK;
+    // ---- scores, transposed: keys 4 grp + i of a block in the lane's registers, query row l16 ----
+    f32x4 s[MQ][NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int key = wk * KW + nb * 16 + l16;
+      const lds_u8* row = kb + key * ROWB;
+#pragma unroll
+      for (int mq = 0; mq < MQ; ++mq) s[mq][nb] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < QS; ++st) {
+        const u32x4 raw = *reinterpret_cast<const lds_u32x4*>(row + (((st * 4 + grp) ^ (key & SWZ)) * 16));
+        const qword kf = __builtin_bit_cast(qword, raw);
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq) {
+          if constexpr (BF16) {
+            s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mq][st], s[mq][nb], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[mq][st][e], s[mq][nb], 0, 0, 0);
+          }
+        }
+      }
+    }
+
+    // ---- which of the tile's keys a row sees ----
+    constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
+    if (cached != kAll) {
+#pragma unroll
+      for (int mq = 0; mq < MQ; ++mq) {
+        uint64_t sees = cached;
+        int row = row_of[mq];
+        auto see = [&](int r) {
+          const uint32_t bit = (uint32_t)(ctx + r - t0);
+          if (bit < (uint32_t)KT) sees |= 1ull << bit;
+        };
+        if (t0 + KT > ctx) {
+          for (int i = 0; i < kMaxStages && row > 0; ++i) {
+            see(row);
+            row = s_up[row];
+          }
+          see(0);
+        }
+        sees >>= wk * KW + grp * 4;
+        const uint32_t word[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!((word[nb / 2] >> ((nb & 1) * 16 + i)) & 1)) s[mq][nb][i] = SPEC_NEG_INF;
+      }
+    }
+
+    // ---- softmax: weights relative to the running maximum ----
+#pragma unroll
+    for (int mq = 0; mq < MQ; ++mq) {
+      float top = s[mq][0][0];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mq][nb][i]);
+      top = groups_max(top) * sc;
+      if (__any(top > m_run[mq])) {
+        const float m_new = fmaxf(m_run[mq], top), keep = __builtin_amdgcn_exp2f(m_run[mq] - m_new);
+        m_run[mq] = m_new;
+        l_run[mq] *= keep;
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[mq][d][i] *= keep;
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mq][nb][i], sc, -m_run[mq]));
+          s[mq][nb][i] = w;
+          l_run[mq] += w;
+        }
+    }
+
+    // ---- values.  The weights are in the place that the product wants them in if the values' keys are taken in the same
+    // order: 4 grp + i of a block, then of the next ----
+    if constexpr (BF16) {
+      auto values = [&](int nb, int d) -> i16x4 {
+        const int key = wk * KW + nb * 16 + grp * 4 + (l16 >> 2), word = (d * 2 + ((l16 & 3) >> 1)) ^ (key & SWZ);
+        // (16 lanes read four keys' 16 elements, and each gets one element of the four keys)
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + key * ROWB + word * 16 + (l16 & 1) * 8));
+      };
+      if constexpr (NB == 1) {
+        i16x4 w[MQ];
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq) {
+          const uint32_t lo = f32_to_bf16_pair(s[mq][0][0], s[mq][0][1]), hi = f32_to_bf16_pair(s[mq][0][2], s[mq][0][3]);
+          w[mq] = __builtin_bit_cast(i16x4, (uint64_t)hi << 32 | lo);
+        }
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+          const i16x4 v = values(0, d);
+#pragma unroll
+          for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, w[mq], o[mq][d], 0, 0, 0);
+        }
+      } else {
+        bf16x8 w[MQ][NB / 2];
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq)
+#pragma unroll
+          for (int j = 0; j < NB / 2; ++j) {
+            const f32x4 a = s[mq][2 * j], b = s[mq][2 * j + 1];
+            const u32x4 raw = {f32_to_bf16_pair(a[0], a[1]), f32_to_bf16_pair(a[2], a[3]), f32_to_bf16_pair(b[0], b[1]), f32_to_bf16_pair(b[2], b[3])};
+            w[mq][j] = __builtin_bit_cast(bf16x8, raw);
+          }
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+          for (int j = 0; j < NB / 2; ++j) {
+            const i16x4 a = values(2 * j, d), b = values(2 * j + 1, d);
+            const bf16x8 v = __builtin_bit_cast(bf16x8, (i16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[mq][j], o[mq][d], 0, 0, 0);
+          }
+      }
+    } else {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = wk * KW + nb * 16 + grp * 4 + i;
+#pragma unroll
+          for (int d = 0; d < DP / 16; ++d) {
+            const float v = *reinterpret_cast<const lds_f32*>(vb + key * ROWB + ((d * 4 + (l16 >> 2)) ^ (key & SWZ)) * 16 + (l16 & 3) * 4);
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[mq][nb][i], o[mq][d], 0, 0, 0);
+          }
+        }
+    }
+  }
+};
+
+// What a wave needs to find a segment's keys.
+struct KeySource {
+  const uint8_t *k_cache, *k_rows;        // of the head
+  int64_t to_v_cache, to_v_rows;          // from a key to its value
+  const int32_t* table;
+  int ctx, keys, last_word;
+};
+
+// The tiles of a segment.  The next tile is copied into the other buffer while one is worked on; the two buffers are distinct
+// objects to the compiler (restrict), so that a read of one does not wait for the copies into the other.
+template <bool BF16, int DP, int MQ, int WK, int KT>
+struct AttentionLoop {
+  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
+  static constexpr int RW = KT / 4;            // rows of a tile that a wave copies
+  static constexpr int RPI = 64 / S::CH;       // rows per instruction
+  static constexpr int NL = RW / RPI;          // instructions for keys, and for values
+  const AttentionJob& p;
+  const KeySource& src;
+  AttentionTile<BF16, DP, MQ, WK, KT>& tile;
+  uint32_t (*s_valid)[4];
+  const uint16_t* s_up;
+  float sc;
+  int tile0, n_tiles;
+  uint64_t a_next;        // place of this lane's row of the tile that is copied next ...
+  uint32_t valid_next;    // ... and which of the wave's rows of it are cached tokens
+
+  // The place of row lane % RW of the wave's fourth of a tile; bit 0 says that it is not in the cache.
+  __device__ __forceinline__ void place(int t) {
+    const int key = (tile0 + t) * KT + (threadIdx.x >> 6) * RW + (threadIdx.x & 63) % RW;
+    // what is not a key is read from row 0, which every row sees: with a weight of zero it adds nothing
+    uint64_t a = reinterpret_cast<uint64_t>(src.k_rows) | 1;
+    bool ok = false;
+    if (key < src.ctx) {
+      const int b = key / p.block_size, x = src.table[b];
+      if (x >= 0 && x < p.n_blocks) {
+        a = reinterpret_cast<uint64_t>(src.k_cache + x * p.block + (key - b * p.block_size) * p.slot);
+        ok = true;
+      }
+    } else if (key < src.keys) {
+      a = reinterpret_cast<uint64_t>(src.k_rows + (int64_t)(key - src.ctx) * p.new_row) | 1;
+    }
+    a_next = a;
+    valid_next = (uint32_t)__ballot(ok) & (uint32_t)((1ull << RW) - 1);
+  }
+
+  __device__ __forceinline__ void copy(lds_u8* to, int t) {
+    const int tid = opaque_tid(), lane = tid & 63, wave = tid >> 6;
+    if (lane == 0) s_valid[t & 1][wave] = valid_next;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      // (a lane's 16 bytes land at its place in the instruction's 1 KiB: the words of a row are permuted where they are read)
+      const int from = j * RPI + lane / S::CH, word = (lane % S::CH) ^ ((wave * RW + from) & S::SWZ);
+      const uint64_t x = __shfl((unsigned long long)a_next, from);
+      const uint8_t* kp = reinterpret_cast<const uint8_t*>(x & ~1ull) + min(word, src.last_word) * 16;
+      const uint8_t* vp = kp + (x & 1 ? src.to_v_rows : src.to_v_cache);
+      lds_u8* at = to + (wave * RW + j * RPI) * S::ROWB;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)at, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)(at + KT * S::ROWB), 16, 0, 0);
+    }
+  }
+
+  __device__ __forceinline__ void turn(lds_u8* __restrict now, lds_u8* __restrict next, int t) {
+    // this wave's copies have landed, and so have the others'; all are done with the other buffer
+    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
+    __syncthreads();
+    if (t + 1 < n_tiles) copy(next, t + 1);
+    uint64_t cached = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) cached |= (uint64_t)s_valid[t & 1][w] << (w * RW);
+    tile.step(now, now + KT * S::ROWB, cached, (tile0 + t) * KT, src.ctx, s_up, sc);
+    if (t + 2 < n_tiles) place(t + 2);
+  }
+
+  __device__ __forceinline__ void run(lds_u8* b0, lds_u8* b1) {
+    if (n_tiles <= 0) return;
+    place(0);
+    copy(b0, 0);
+    if (n_tiles > 1) place(1);
+    for (int t = 0; t < n_tiles; t += 2) {
+      turn(b0, b1, t);
+      if (t + 1 < n_tiles) turn(b1, b0, t + 1);
+    }
+  }
+};
+
 template <bool BF16, int DP, int MQ, int WK, int KT>
 __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 ? 2 : 1) void attention_kernel(AttentionJob p, AttentionSpace ws) {
   typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
-  constexpr int ESZ = S::ESZ, ROWB = S::ROWB, CH = S::CH, BM = S::BM, KW = S::KW, NB = S::NB, SWZ = S::SWZ;
-  constexpr int RW = KT / 4;            // rows of a tile that a wave loads
-  constexpr int RPI = 64 / CH;          // rows per instruction
-  constexpr int NL = RW / RPI;          // instructions for keys, and for values
-  constexpr int QS = BF16 ? DP / 32 : DP / 16;   // steps along the head
+  typedef AttentionTile<BF16, DP, MQ, WK, KT> Tile;
+  constexpr int ESZ = S::ESZ, BM = S::BM;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + S::LDS);   // [M + 1]: row of a row's parent
   __shared__ uint32_t s_valid[2][4];
@@ -108,13 +354,14 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   }
   // (consecutive shares, which meet in the same keys, run on the same XCD)
   const int me = (int)(blockIdx.x % 8) * (ws.groups / 8) + (int)(blockIdx.x / 8);
+  all = uniform(all);
   const uint64_t groups = min((uint64_t)ws.groups, (all + ws.least - 1) / ws.least);
   if (me >= (int)groups) {
     if (tid == 0) ws.owner[me].q = -1;
     return;
   }
-  uint64_t at = all * me / groups;
-  const uint64_t end = all * (me + 1) / groups;
+  uint64_t at = uniform(all * me / groups);
+  const uint64_t end = uniform(all * (me + 1) / groups);
   int q = 0;
   uint64_t start = 0;   // of sequence q
   for (int q0 = 0;; q0 += 64) {
@@ -127,14 +374,18 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     const uint64_t over = __ballot(start + sum > at);
     if (over) {
       const int l = __ffsll((unsigned long long)over) - 1;
-      q = q0 + l;
-      start += __shfl((unsigned long long)(sum - t), l);
+      q = uniform(q0 + l);
+      start = uniform(start + (uint64_t)__shfl((unsigned long long)(sum - t), l));
       break;
     }
-    start += __shfl((unsigned long long)sum, 63);
+    start = uniform(start + (uint64_t)__shfl((unsigned long long)sum, 63));
   }
   Owner mine = {-1, 0, 0, 0};
-  SeqTiles sq = seq_tiles<KT>(p, q, BM);
+  SeqTiles sq = seq_tiles<KT, true>(p, q, BM);
+  // the first segment's place; the others start at the next unit's first tile
+  uint64_t unit = uniform((at - start) / (uint64_t)sq.tiles);
+  int tile0 = uniform((int)(at - start - unit * (uint64_t)sq.tiles));
+  int g = uniform((int)(unit / (uint64_t)sq.blocks)), block = uniform((int)(unit - (uint64_t)g * (uint64_t)sq.blocks));
 
   // a negative scale goes into the queries' sign, a scale of zero makes them zero: the largest product has the largest weight
   const float q_sign = p.scale < 0 ? -1.0f : p.scale == 0 ? 0.0f : 1.0f;
@@ -142,36 +393,33 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   const int last_word = p.head_dim * ESZ / 16 - 1;
 
   while (at < end) {
-    while (at >= start + sq.total) {
-      start += sq.total;
-      sq = seq_tiles<KT>(p, ++q, BM);
-    }
-    const uint64_t local = at - start, unit = local / (uint64_t)sq.tiles;
-    const int tile0 = (int)(local - unit * (uint64_t)sq.tiles), g = (int)(unit / (uint64_t)sq.blocks);
-    const int block = (int)(unit - (uint64_t)g * (uint64_t)sq.blocks);
     const int n_seg = (int)min(end - at, (uint64_t)(sq.tiles - tile0));
-    const int ctx = sq.ctx, rows = (sq.nodes + 1) * G - block * BM;            // query rows from this unit's first on
+    const int rows = (sq.nodes + 1) * G - block * BM;                          // query rows from this unit's first on
     const int last_row = min(sq.nodes, (block * BM + BM - 1) / G);             // its last tree row
-    const int keys = ctx + last_row + 1;                                       // what it sees at most
-    const int n_tiles = min(n_seg, (keys + KT - 1) / KT - tile0);              // (tiles behind that: rows that are nobody's ancestor)
+    KeySource src;
+    src.ctx = sq.ctx;
+    src.keys = sq.ctx + last_row + 1;                                          // what it sees at most
+    src.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)g * p.cache_head;
+    src.k_rows = static_cast<const uint8_t*>(p.k_new) + q * p.new_seq + (int64_t)g * p.new_head;
+    src.to_v_cache = static_cast<const uint8_t*>(p.v) - static_cast<const uint8_t*>(p.k);
+    src.to_v_rows = static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new);
+    src.table = p.block_table + (int64_t)q * p.max_blocks;
+    src.last_word = last_word;
+    const int n_tiles = min(n_seg, (src.keys + KT - 1) / KT - tile0);          // (tiles behind that: rows that are nobody's ancestor)
     __syncthreads();   // the last unit is done with the memory
-    if ((tile0 + n_tiles) * KT > ctx)
+    if ((tile0 + n_tiles) * KT > sq.ctx)
       for (int i = tid; i < last_row; i += 256) {
         const int up = p.node_parent[(int64_t)q * p.M + i];
         s_up[i + 1] = (uint16_t)(up >= 0 && up < i ? up + 1 : 0);
       }
-
-    // ---- queries: lane l16 of every group holds row l16 of each block of 16 ----
-    typedef typename std::conditional<BF16, bf16x8, f32x4>::type qword;
-    qword qf[MQ][QS];
-    int row_of[MQ];
+    Tile x;
 #pragma unroll
     for (int mq = 0; mq < MQ; ++mq) {
       const int m = (wq * MQ + mq) * 16 + l16, mm = m < rows ? block * BM + m : 0;
-      row_of[mq] = mm / G;
-      const uint8_t* from = static_cast<const uint8_t*>(p.q) + q * p.q_seq + (int64_t)row_of[mq] * p.q_row + (int64_t)(g * G + mm % G) * p.q_head;
+      x.row_of[mq] = mm / G;
+      const uint8_t* from = static_cast<const uint8_t*>(p.q) + q * p.q_seq + (int64_t)x.row_of[mq] * p.q_row + (int64_t)(g * G + mm % G) * p.q_head;
 #pragma unroll
-      for (int s = 0; s < QS; ++s) {
+      for (int s = 0; s < Tile::QS; ++s) {
         const int word = s * 4 + grp;
         u32x4 raw = {0, 0, 0, 0};
         if (word <= last_word) raw = *reinterpret_cast<const u32x4*>(from + word * 16);
@@ -179,219 +427,17 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 #pragma unroll
           for (int i = 0; i < 4; ++i) raw[i] = q_sign == 0.0f ? 0u : raw[i] ^ (BF16 ? 0x80008000u : 0x80000000u);
         }
-        qf[mq][s] = __builtin_bit_cast(qword, raw);
+        x.qf[mq][s] = __builtin_bit_cast(typename Tile::qword, raw);
       }
+      x.m_run[mq] = kLowest;
+      x.l_run[mq] = 0;
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) x.o[mq][d] = (f32x4){0, 0, 0, 0};
     }
-    f32x4 o[MQ][DP / 16];
-    float m_run[MQ], l_run[MQ];
+    AttentionLoop<BF16, DP, MQ, WK, KT> loop = {p, src, x, s_valid, s_up, sc, tile0, n_tiles, 0, 0};
+    loop.run((lds_u8*)smem, (lds_u8*)(smem + S::LDS / 2));
 #pragma unroll
-    for (int mq = 0; mq < MQ; ++mq) {
-      m_run[mq] = kLowest;
-      l_run[mq] = 0;
-#pragma unroll
-      for (int d = 0; d < DP / 16; ++d) o[mq][d] = (f32x4){0, 0, 0, 0};
-    }
-
-    // ---- keys and values: a wave loads a fourth of a tile's rows.  A lane finds the place of row lane % RW; bit 0 of the
-    // address says that it is not in the cache ----
-    const uint8_t* k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)g * p.cache_head;
-    const uint8_t* k_rows = static_cast<const uint8_t*>(p.k_new) + q * p.new_seq + (int64_t)g * p.new_head;
-    const int64_t to_v_cache = static_cast<const uint8_t*>(p.v) - static_cast<const uint8_t*>(p.k);
-    const int64_t to_v_rows = static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new);
-    const int32_t* table = p.block_table + (int64_t)q * p.max_blocks;
-    auto place = [&](int tile, uint32_t& valid) -> uint64_t {
-      const int key = tile * KT + wave * RW + lane % RW;
-      // what is not a key is read from row 0, which every row sees: with a weight of zero it adds nothing
-      uint64_t a = reinterpret_cast<uint64_t>(k_rows) | 1;
-      bool ok = false;
-      if (key < ctx) {
-        const int b = key / p.block_size, x = table[b];
-        if (x >= 0 && x < p.n_blocks) {
-          a = reinterpret_cast<uint64_t>(k_cache + x * p.block + (key - b * p.block_size) * p.slot);
-          ok = true;
-        }
-      } else if (key < keys) {
-        a = reinterpret_cast<uint64_t>(k_rows + (int64_t)(key - ctx) * p.new_row) | 1;
-      }
-      valid = (uint32_t)__ballot(ok) & (uint32_t)((1ull << RW) - 1);
-      return a;
-    };
-    u32x4 kr[NL], vr[NL];
-    auto load = [&](uint64_t a) {
-#pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        const int from = j * RPI + lane / CH, word = (lane % CH) ^ ((wave * RW + from) & SWZ);
-        const uint64_t x = __shfl((unsigned long long)a, from);
-        const uint8_t* kp = reinterpret_cast<const uint8_t*>(x & ~1ull) + min(word, last_word) * 16;
-        kr[j] = *reinterpret_cast<const u32x4*>(kp);
-        vr[j] = *reinterpret_cast<const u32x4*>(kp + (x & 1 ? to_v_rows : to_v_cache));
-      }
-    };
-    uint32_t valid = 0, valid_next = 0;
-    uint64_t a_next = 0;
-    if (n_tiles > 0) {
-      const uint64_t a = place(tile0, valid);
-      load(a);
-      if (n_tiles > 1) a_next = place(tile0 + 1, valid_next);
-    }
-    for (int t = 0; t < n_tiles; ++t) {
-      uint8_t* kb = smem + (t & 1) * 2 * KT * ROWB;
-      uint8_t* vb = kb + KT * ROWB;
-#pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        const int to = (wave * RW + j * RPI) * ROWB + lane * 16;
-        *reinterpret_cast<u32x4*>(kb + to) = kr[j];
-        *reinterpret_cast<u32x4*>(vb + to) = vr[j];
-      }
-      if (lane == 0) s_valid[t & 1][wave] = valid;
-      __syncthreads();   // (the buffer written next was last read before the previous barrier)
-      if (t + 1 < n_tiles) load(a_next);
-
-      // ---- scores, transposed: keys 4 grp + i of a block in the lane's registers, query row l16 ----
-      f32x4 s[MQ][NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int key = wk * KW + nb * 16 + l16;
-        const uint8_t* row = kb + key * ROWB;
-#pragma unroll
-        for (int mq = 0; mq < MQ; ++mq) s[mq][nb] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < QS; ++st) {
-          const u32x4 raw = *reinterpret_cast<const u32x4*>(row + (((st * 4 + grp) ^ (key & SWZ)) * 16));
-          const qword kf = __builtin_bit_cast(qword, raw);
-#pragma unroll
-          for (int mq = 0; mq < MQ; ++mq) {
-            if constexpr (BF16) {
-              s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mq][st], s[mq][nb], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[mq][st][e], s[mq][nb], 0, 0, 0);
-            }
-          }
-        }
-      }
-
-      // ---- which of the tile's keys a row sees ----
-      const int t0 = (tile0 + t) * KT;
-      uint64_t cached = 0;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) cached |= (uint64_t)s_valid[t & 1][w] << (w * RW);
-      constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
-      if (cached != kAll) {
-#pragma unroll
-        for (int mq = 0; mq < MQ; ++mq) {
-          uint64_t sees = cached;
-          int row = row_of[mq];
-          auto see = [&](int r) {
-            const uint32_t bit = (uint32_t)(ctx + r - t0);
-            if (bit < (uint32_t)KT) sees |= 1ull << bit;
-          };
-          if (t0 + KT > ctx) {
-            for (int i = 0; i < kMaxStages && row > 0; ++i) {
-              see(row);
-              row = s_up[row];
-            }
-            see(0);
-          }
-          const uint32_t mine_ = (uint32_t)(sees >> (wk * KW + grp * 4) & 0xffffffffull), above = (uint32_t)(sees >> (wk * KW + grp * 4) >> 32);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t word = nb < 2 ? mine_ : above;
-              if (!((word >> ((nb & 1) * 16 + i)) & 1)) s[mq][nb][i] = SPEC_NEG_INF;
-            }
-        }
-      }
-
-      // ---- softmax: weights relative to the running maximum ----
-#pragma unroll
-      for (int mq = 0; mq < MQ; ++mq) {
-        float top = s[mq][0][0];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mq][nb][i]);
-        top = groups_max(top) * sc;
-        if (__any(top > m_run[mq])) {
-          const float m_new = fmaxf(m_run[mq], top), keep = __builtin_amdgcn_exp2f(m_run[mq] - m_new);
-          m_run[mq] = m_new;
-          l_run[mq] *= keep;
-#pragma unroll
-          for (int d = 0; d < DP / 16; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[mq][d][i] *= keep;
-        }
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mq][nb][i], sc, -m_run[mq]));
-            s[mq][nb][i] = w;
-            l_run[mq] += w;
-          }
-      }
-
-      // ---- values: o transposed, elements 16 d + 4 grp + i of the head, query row l16.  The weights are in the place that the
-      // product wants them in if the values' keys are taken in the same order: 4 grp + i of a block, then of the next ----
-      if constexpr (BF16) {
-        auto values = [&](int nb, int d) -> i16x4 {
-          const int key = wk * KW + nb * 16 + grp * 4 + (l16 >> 2), word = (d * 2 + ((l16 & 3) >> 1)) ^ (key & SWZ);
-          // (16 lanes read four keys' 16 elements, and each gets one element of the four keys)
-          return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + key * ROWB + word * 16 + (l16 & 1) * 8));
-        };
-        if constexpr (NB == 1) {
-          i16x4 w[MQ];
-#pragma unroll
-          for (int mq = 0; mq < MQ; ++mq) {
-            const uint32_t lo = f32_to_bf16_pair(s[mq][0][0], s[mq][0][1]), hi = f32_to_bf16_pair(s[mq][0][2], s[mq][0][3]);
-            w[mq] = __builtin_bit_cast(i16x4, (uint64_t)hi << 32 | lo);
-          }
-#pragma unroll
-          for (int d = 0; d < DP / 16; ++d) {
-            const i16x4 v = values(0, d);
-#pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, w[mq], o[mq][d], 0, 0, 0);
-          }
-        } else {
-          bf16x8 w[MQ][NB / 2];
-#pragma unroll
-          for (int mq = 0; mq < MQ; ++mq)
-#pragma unroll
-            for (int j = 0; j < NB / 2; ++j) {
-              const f32x4 a = s[mq][2 * j], b = s[mq][2 * j + 1];
-              const u32x4 raw = {f32_to_bf16_pair(a[0], a[1]), f32_to_bf16_pair(a[2], a[3]), f32_to_bf16_pair(b[0], b[1]), f32_to_bf16_pair(b[2], b[3])};
-              w[mq][j] = __builtin_bit_cast(bf16x8, raw);
-            }
-#pragma unroll
-          for (int d = 0; d < DP / 16; ++d)
-#pragma unroll
-            for (int j = 0; j < NB / 2; ++j) {
-              const i16x4 a = values(2 * j, d), b = values(2 * j + 1, d);
-              const bf16x8 v = __builtin_bit_cast(bf16x8, (i16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
-#pragma unroll
-              for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[mq][j], o[mq][d], 0, 0, 0);
-            }
-        }
-      } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = wk * KW + nb * 16 + grp * 4 + i;
-#pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-              const float v = *reinterpret_cast<const float*>(vb + key * ROWB + ((d * 4 + (l16 >> 2)) ^ (key & SWZ)) * 16 + (l16 & 3) * 4);
-#pragma unroll
-              for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[mq][nb][i], o[mq][d], 0, 0, 0);
-            }
-          }
-      }
-      valid = valid_next;
-      if (t + 2 < n_tiles) a_next = place(tile0 + t + 2, valid_next);
-    }
-#pragma unroll
-    for (int mq = 0; mq < MQ; ++mq) l_run[mq] = groups_sum(l_run[mq]);
+    for (int mq = 0; mq < MQ; ++mq) x.l_run[mq] = groups_sum(x.l_run[mq]);
 
     // ---- join of the waves that took other keys of the same rows ----
     if constexpr (WK > 1) {
@@ -402,12 +448,12 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         float* to = box + ((wk - 1) * S::WQ + wq) * PER * 64 + lane;
 #pragma unroll
         for (int mq = 0; mq < MQ; ++mq) {
-          to[(mq * (DP / 4 + 2)) * 64] = m_run[mq];
-          to[(mq * (DP / 4 + 2) + 1) * 64] = l_run[mq];
+          to[(mq * (DP / 4 + 2)) * 64] = x.m_run[mq];
+          to[(mq * (DP / 4 + 2) + 1) * 64] = x.l_run[mq];
 #pragma unroll
           for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[(mq * (DP / 4 + 2) + 2 + d * 4 + i) * 64] = o[mq][d][i];
+            for (int i = 0; i < 4; ++i) to[(mq * (DP / 4 + 2) + 2 + d * 4 + i) * 64] = x.o[mq][d][i];
         }
       }
       __syncthreads();
@@ -416,14 +462,14 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
           const float* from = box + (w * S::WQ + wq) * PER * 64 + lane;
 #pragma unroll
           for (int mq = 0; mq < MQ; ++mq) {
-            const float m = from[(mq * (DP / 4 + 2)) * 64], m_new = fmaxf(m, m_run[mq]);
-            const float mine_ = __builtin_amdgcn_exp2f(m_run[mq] - m_new), its = __builtin_amdgcn_exp2f(m - m_new);
-            m_run[mq] = m_new;
-            l_run[mq] = l_run[mq] * mine_ + from[(mq * (DP / 4 + 2) + 1) * 64] * its;
+            const float m = from[(mq * (DP / 4 + 2)) * 64], m_new = fmaxf(m, x.m_run[mq]);
+            const float mine_ = __builtin_amdgcn_exp2f(x.m_run[mq] - m_new), its = __builtin_amdgcn_exp2f(m - m_new);
+            x.m_run[mq] = m_new;
+            x.l_run[mq] = x.l_run[mq] * mine_ + from[(mq * (DP / 4 + 2) + 1) * 64] * its;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[mq][d][i] = o[mq][d][i] * mine_ + from[(mq * (DP / 4 + 2) + 2 + d * 4 + i) * 64] * its;
+              for (int i = 0; i < 4; ++i) x.o[mq][d][i] = x.o[mq][d][i] * mine_ + from[(mq * (DP / 4 + 2) + 2 + d * 4 + i) * 64] * its;
           }
         }
       }
@@ -432,34 +478,43 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     // ---- out, or what has been summed so far ----
     const bool whole = n_seg == sq.tiles;
     if (!whole && tile0 == 0)   // the unit ends in the workgroup that takes its last tile
-      mine = {q, g, block, (int)(((start + (unit + 1) * (uint64_t)sq.tiles) * groups - 1) / all)};
+      mine = {q, g, block, (int)(((at + (uint64_t)sq.tiles) * groups - 1) / all)};
     if (wk == 0) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
         const int m = (wq * MQ + mq) * 16 + l16;
         if (m < rows) {
           if (whole) {
-            const float inv = 1.0f / l_run[mq];
-            uint8_t* to = static_cast<uint8_t*>(p.out) + q * p.out_seq + (int64_t)row_of[mq] * p.out_row + (int64_t)(g * G + (block * BM + m) % G) * p.out_head;
+            const float inv = 1.0f / x.l_run[mq];
+            uint8_t* to = static_cast<uint8_t*>(p.out) + q * p.out_seq + (int64_t)x.row_of[mq] * p.out_row + (int64_t)(g * G + (block * BM + m) % G) * p.out_head;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
               const int e = d * 16 + grp * 4;
               if (e < p.head_dim) {
-                const f32x4 x = o[mq][d] * inv;
-                if constexpr (BF16) *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(x[2], x[3]) << 32 | f32_to_bf16_pair(x[0], x[1]);
-                else *reinterpret_cast<f32x4*>(to + e * 4) = x;
+                const f32x4 v = x.o[mq][d] * inv;
+                if constexpr (BF16) *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(v[2], v[3]) << 32 | f32_to_bf16_pair(v[0], v[1]);
+                else *reinterpret_cast<f32x4*>(to + e * 4) = v;
               }
             }
           } else {
             float* to = ws.part + ((int64_t)(me * 2 + (tile0 == 0 ? 1 : 0)) * BM + m) * (DP + 4);
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<f32x4*>(to + d * 16 + grp * 4) = o[mq][d];
-            if (grp == 0) to[DP] = m_run[mq], to[DP + 1] = l_run[mq];
+            for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<f32x4*>(to + d * 16 + grp * 4) = x.o[mq][d];
+            if (grp == 0) to[DP] = x.m_run[mq], to[DP + 1] = x.l_run[mq];
           }
         }
       }
     }
     at += n_seg;
+    tile0 = 0;
+    if (++block == sq.blocks) {
+      block = 0;
+      if (++g == p.kv_heads && at < end) {
+        g = 0;
+        do sq = seq_tiles<KT, true>(p, ++q, BM);
+        while (sq.total == 0);
+      }
+    }
   }
   if (tid == 0) ws.owner[me] = mine;
 }
@@ -494,6 +549,75 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, Att
   }
 }
 
+// float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): one workgroup per
+// (row, query head, sequence), whose four waves take every fourth key, four elements of a row per lane, with
+// the running maximum and sum of the softmax, and are joined at the end.
+__global__ __launch_bounds__(256) void attention_f32_kernel(AttentionJob p) {
+  __shared__ float s_m[4], s_l[4], s_o[4][256];
+  __shared__ int s_row[kMaxStages + 1], s_rows;
+  const int r = blockIdx.x, h = blockIdx.y, q = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int nodes = p.n_nodes ? min(max(p.n_nodes[q], -1), p.M) : p.M;
+  if (r > nodes) return;
+  const int g = h / (p.q_heads / p.kv_heads), ctx = min(max(p.ctx_len[q], 0), p.max_blocks * p.block_size);
+  if (tid == 0) {
+    int n = 0;
+    for (int node = r - 1; node >= 0 && n < kMaxStages;) {
+      s_row[n++] = node + 1;
+      const int up = p.node_parent[(int64_t)q * p.M + node];
+      node = up < node ? up : -1;
+    }
+    s_row[n++] = 0;
+    s_rows = n;
+  }
+  __syncthreads();
+  const float* qr = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.q) + q * p.q_seq + r * p.q_row + h * p.q_head);
+  float x[4], o[4] = {0, 0, 0, 0}, m = kLowest, l = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = lane + i * 64 < p.head_dim ? qr[lane + i * 64] * p.scale : 0.0f;
+  const int keys = ctx + s_rows;
+  for (int t = wave; t < keys; t += 4) {
+    const float *k, *v;
+    if (t < ctx) {
+      const int b = p.block_table[(int64_t)q * p.max_blocks + t / p.block_size];
+      if (b < 0 || b >= p.n_blocks) continue;
+      const int64_t at = b * p.block + t % p.block_size * p.slot + g * p.cache_head;
+      k = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.k) + at);
+      v = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.v) + at);
+    } else {
+      const int64_t at = q * p.new_seq + s_row[t - ctx] * p.new_row + g * p.new_head;
+      k = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.k_new) + at);
+      v = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.v_new) + at);
+    }
+    float s = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (lane + i * 64 < p.head_dim) s += x[i] * k[lane + i * 64];
+    s = wave_sum(s);
+    const float top = fmaxf(m, s), w = expf(s - top), keep = expf(m - top);
+    l = l * keep + w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (lane + i * 64 < p.head_dim) o[i] = o[i] * keep + w * v[lane + i * 64];
+    m = top;
+  }
+  if (lane == 0) s_m[wave] = m, s_l[wave] = l;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s_o[wave][lane + i * 64] = o[i];
+  __syncthreads();
+  // (row 0 is always there: one of the four has a key)
+  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  float sum = 0, val = 0;
+  for (int w = 0; w < 4; ++w) {
+    const float f = expf(s_m[w] - top);
+    sum += f * s_l[w];
+    val += f * s_o[w][tid];
+  }
+  if (tid < p.head_dim) {
+    uint8_t* to = static_cast<uint8_t*>(p.out) + q * p.out_seq + r * p.out_row + h * p.out_head;
+    reinterpret_cast<float*>(to)[tid] = val / sum;
+  }
+}
+
 // Query rows of a key/value head: at most 16, the waves share the keys; at most 32, by twos; more, each has rows of its own.
 struct AttentionPlan {
   int dp, bm, groups, least;
@@ -503,8 +627,8 @@ static AttentionPlan plan_attention(int M, int q_heads, int kv_heads, int head_d
   a.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)(M + 1) * (q_heads / kv_heads);
   a.bm = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || a.dp == 256 || !bf16 ? 64 : 128;
-  if (!bf16 && a.dp == 256 && a.bm == 16) a.bm = 32;
   a.groups = a.dp * (bf16 ? 1 : 2) <= 128 ? 512 : 256;   // two workgroups of 64 KiB fit a CU
+  if (!bf16 && a.dp == 256) a.groups = 0;
   a.least = 2;
   return a;
 }
@@ -542,6 +666,10 @@ static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPla
 
 hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st) {
   const AttentionPlan a = plan_attention(job.M, job.q_heads, job.kv_heads, job.head_dim, bf16);
+  if (a.groups == 0) {
+    hipLaunchKernelGGL(attention_f32_kernel, dim3(job.M + 1, job.q_heads, job.batch), dim3(256), 0, st, job);
+    return hipGetLastError();
+  }
 #define LAUNCH(BF16, DP, BM, MQ, WK, KT) \
   if (bf16 == BF16 && a.dp == DP && a.bm == BM) return launch_attention_t<BF16, DP, MQ, WK, KT>(job, a, st)
   LAUNCH(true, 64, 16, 1, 4, 64);
@@ -561,8 +689,6 @@ hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st) 
   LAUNCH(false, 128, 16, 1, 4, 64);
   LAUNCH(false, 128, 32, 1, 2, 64);
   LAUNCH(false, 128, 64, 1, 1, 64);
-  LAUNCH(false, 256, 32, 1, 2, 32);
-  LAUNCH(false, 256, 64, 1, 1, 32);
 #undef LAUNCH
   return hipErrorInvalidValue;
 }

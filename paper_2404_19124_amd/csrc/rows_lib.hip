@@ -38,7 +38,7 @@ static spec_status_t check_attention_shape(int32_t batch, int32_t M, int32_t q_h
   if (batch < 1 || M < 0 || q_heads < 1) return fail(SPEC_EINVAL, "batch and q_heads must be >= 1, M >= 0");
   if (q_heads % kv_heads) return fail(SPEC_ESHAPE, "q_heads = %d is not a multiple of kv_heads = %d", q_heads, kv_heads);
   if (M > kMaxTreeItems) return fail(SPEC_ESHAPE, "M = %d exceeds %d", M, kMaxTreeItems);
-  if ((int64_t)batch * kv_heads >= 1 << 24 || q_heads / kv_heads >= 1 << 16) return fail(SPEC_ESHAPE, "too many heads for one call");
+  if (batch > 65535 || q_heads > 65535) return fail(SPEC_ESHAPE, "batch = %d or q_heads = %d exceeds 65535", batch, q_heads);
   return SPEC_OK;
 }
 
