@@ -3,7 +3,7 @@
 // over the cached tokens and the rows 0, the ancestors of r, and r.
 //
 // A UNIT is BM query rows of one key/value head of one sequence: the rows of all query heads that share it, tree row by tree
-// row.  Its keys are the cached tokens and then the sequence's rows, in TILES of KT.  One pass over the tiles keeps, per
+// row.  Its keys are the cached tokens and then the sequence's rows, in TILES of 64.  One pass over the tiles keeps, per
 // query row, the running maximum m, sum l of the softmax's weights and the weighted sum o of the values (with a larger
 // maximum m', l and o are multiplied by exp(m - m')).
 #include <atomic>
@@ -23,6 +23,7 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int KT = 64;   // keys of a tile
 
 // larger / sum of a value and those of the lanes 16 and 32 away: the same query row's other keys
 __device__ __forceinline__ float groups_max(float x) {
@@ -53,7 +54,7 @@ struct SeqTiles {
   int ctx, nodes, tiles, blocks;   // cached tokens, last row, tiles per unit, units per key/value head
   uint64_t total;                  // tiles of all units
 };
-template <int KT, bool UNIFORM = false>
+template <bool UNIFORM = false>
 __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int BM) {
   SeqTiles s;
   int ctx = p.ctx_len[q], nodes = p.n_nodes ? p.n_nodes[q] : p.M;
@@ -82,22 +83,21 @@ struct AttentionSpace {
 // two buffers of keys and values
 constexpr int tile_bytes(int one) { return 4 * one; }
 
-template <bool BF16, int DP, int MQ, int WK, int KT>
+template <bool BF16, int DP, int MQ, int WK>
 struct AttentionShape {
   static constexpr int ESZ = BF16 ? 2 : 4, ROWB = DP * ESZ, CH = ROWB / 16;   // bytes and 16-byte words of a row
   static constexpr int WQ = 4 / WK, BM = 16 * MQ * WQ;                        // waves along the query rows; query rows of a unit
   static constexpr int KW = KT / WK, NB = KW / 16;                            // keys of a wave, blocks of 16 of them
   static constexpr int LDS = tile_bytes(KT * ROWB);
   static constexpr int SWZ = CH < 16 ? CH - 1 : 15;
-  static_assert(KW % 16 == 0 && KT % 4 == 0, "a wave takes whole blocks of keys, and loads a fourth of a tile");
-  // joins of the waves that share query rows go through the tiles' memory
-  static_assert((WK - 1) * WQ * 64 * MQ * (DP / 4 + 2) * 4 <= LDS, "the waves' results fit the tiles' memory");
+  // joins of the waves that share query rows go through the memory of one tile
+  static_assert((WK - 1) * WQ * 64 * MQ * (DP / 4 + 2) * 4 <= LDS / 2, "the waves' results fit a tile's memory");
 };
 
 // One tile of one unit: scores, softmax and values of a wave's keys and query rows.
-template <bool BF16, int DP, int MQ, int WK, int KT>
+template <bool BF16, int DP, int MQ, int WK>
 struct AttentionTile {
-  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
   typedef typename std::conditional<BF16, bf16x8, f32x4>::type qword;
   static constexpr int QS = BF16 ? DP / 32 : DP / 16;   // steps along the head
   qword qf[MQ][QS];       // queries: lane l16 of every group holds row l16 of each block of 16
@@ -134,8 +134,7 @@ struct AttentionTile {
     }
 
     // ---- which of the tile's keys a row sees ----
-    constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
-    if (cached != kAll) {
+    if (cached != ~0ull) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
         uint64_t sees = cached;
@@ -247,98 +246,142 @@ struct AttentionTile {
   }
 };
 
-// What a wave needs to find a segment's keys.
-struct KeySource {
-  const uint8_t *k_cache, *k_rows;        // of the head
-  int64_t to_v_cache, to_v_rows;          // from a key to its value
-  const int32_t* table;
-  int ctx, keys, last_word;
+// One turn of a workgroup: tile `cur` has landed; the next one is copied into `other` while it is worked on.
+template <bool BF16, int DP, int MQ, int WK, typename Copy>
+__device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& x, lds_u8* __restrict cur, lds_u8* __restrict other, const uint32_t* valid,
+                                               int t0, int ctx, const uint16_t* s_up, float sc, Copy&& copy_next) {
+  // this wave's copies have landed, and behind the barrier the others'; all are done with the other buffer
+  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
+  __syncthreads();
+  copy_next(other);
+  uint64_t cached = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) cached |= (uint64_t)valid[w] << (w * (KT / 4));
+  x.step(cur, cur + KT * AttentionShape<BF16, DP, MQ, WK>::ROWB, cached, t0, ctx, s_up, sc);
+}
+
+// A unit's tiles that a workgroup takes, in scalar registers.
+struct Segment {
+  int q, g, block;                   // sequence, key/value head, block of BM query rows
+  int ctx, nodes, tiles, blocks;     // as SeqTiles
+  int tile0, n_seg, n_tiles;         // first tile, tiles, and those of them that hold keys of its rows (at least one)
+  int keys;                          // cached tokens and rows up to its last one
+  const uint8_t *k_cache, *k_rows;   // of the head
 };
 
-// The tiles of a segment.  The next tile is copied into the other buffer while one is worked on; the two buffers are distinct
-// objects to the compiler (restrict), so that a read of one does not wait for the copies into the other.
-template <bool BF16, int DP, int MQ, int WK, int KT>
-struct AttentionLoop {
-  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
-  static constexpr int RW = KT / 4;            // rows of a tile that a wave copies
-  static constexpr int RPI = 64 / S::CH;       // rows per instruction
+// How a workgroup copies tiles into LDS, one ahead of the one it works on, across its segments.  A wave copies a fourth of a
+// tile's rows, 1 KiB (RPI rows) per instruction.  Where the wave's 16 tokens lie in one page, their place is one address for all
+// lanes, and the lanes' offsets from it are the same for every tile: it is found for 64 tiles at once, a tile per lane.
+// Otherwise (rows of the tree, the last cached tokens, pages of other sizes, blocks out of range) lane l finds the place of row
+// l % 16.  (The second way for every tile: 154 vector instructions per tile instead of 30.)
+template <bool BF16, int DP, int MQ, int WK>
+struct TileCopy {
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
+  static constexpr int RW = KT / 4;
+  static constexpr int RPI = 64 / S::CH;
   static constexpr int NL = RW / RPI;          // instructions for keys, and for values
   const AttentionJob& p;
-  const KeySource& src;
-  AttentionTile<BF16, DP, MQ, WK, KT>& tile;
   uint32_t (*s_valid)[4];
-  const uint16_t* s_up;
-  float sc;
-  int tile0, n_tiles;
-  uint64_t a_next;        // place of this lane's row of the tile that is copied next ...
-  uint32_t valid_next;    // ... and which of the wave's rows of it are cached tokens
+  int last_word;
+  int64_t to_v_cache, to_v_rows;               // from a key to its value
+  uint32_t offset[NL];                         // of this lane's words from the place of the wave's rows
+  // for the segment that is worked on and for the one behind it: offsets into the cache of the wave's rows of 64 tiles from
+  // tile `base` on (lane by lane, -1: no single place)
+  struct Places {
+    int64_t at;
+    int base;
+  };
+  // the tile that is copied next, where it has no single place: this lane's address (bit 0: not in the cache) and which of
+  // the wave's rows are cached tokens
+  struct Rows {
+    uint64_t at;
+    uint32_t valid;
+  };
 
-  // The place of row lane % RW of the wave's fourth of a tile; bit 0 says that it is not in the cache.
-  __device__ __forceinline__ void place(int t) {
-    const int key = (tile0 + t) * KT + (threadIdx.x >> 6) * RW + (threadIdx.x & 63) % RW;
-    // what is not a key is read from row 0, which every row sees: with a weight of zero it adds nothing
-    uint64_t a = reinterpret_cast<uint64_t>(src.k_rows) | 1;
-    bool ok = false;
-    if (key < src.ctx) {
-      const int b = key / p.block_size, x = src.table[b];
-      if (x >= 0 && x < p.n_blocks) {
-        a = reinterpret_cast<uint64_t>(src.k_cache + x * p.block + (key - b * p.block_size) * p.slot);
-        ok = true;
-      }
-    } else if (key < src.keys) {
-      a = reinterpret_cast<uint64_t>(src.k_rows + (int64_t)(key - src.ctx) * p.new_row) | 1;
-    }
-    a_next = a;
-    valid_next = (uint32_t)__ballot(ok) & (uint32_t)((1ull << RW) - 1);
-  }
-
-  __device__ __forceinline__ void copy(lds_u8* to, int t) {
-    const int tid = opaque_tid(), lane = tid & 63, wave = tid >> 6;
-    if (lane == 0) s_valid[t & 1][wave] = valid_next;
+  __device__ __forceinline__ void init() {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      // (a lane's 16 bytes land at its place in the instruction's 1 KiB: the words of a row are permuted where they are read)
-      const int from = j * RPI + lane / S::CH, word = (lane % S::CH) ^ ((wave * RW + from) & S::SWZ);
-      const uint64_t x = __shfl((unsigned long long)a_next, from);
-      const uint8_t* kp = reinterpret_cast<const uint8_t*>(x & ~1ull) + min(word, src.last_word) * 16;
-      const uint8_t* vp = kp + (x & 1 ? src.to_v_rows : src.to_v_cache);
-      lds_u8* at = to + (wave * RW + j * RPI) * S::ROWB;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)at, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)(at + KT * S::ROWB), 16, 0, 0);
+      const int row = j * RPI + lane / S::CH, word = (lane % S::CH) ^ ((wave * RW + row) & S::SWZ);
+      offset[j] = (uint32_t)(row * (int)p.slot + min(word, last_word) * 16);
     }
   }
 
-  __device__ __forceinline__ void turn(lds_u8* __restrict now, lds_u8* __restrict next, int t) {
-    // this wave's copies have landed, and so have the others'; all are done with the other buffer
-    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
-    __syncthreads();
-    if (t + 1 < n_tiles) copy(next, t + 1);
-    uint64_t cached = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) cached |= (uint64_t)s_valid[t & 1][w] << (w * RW);
-    tile.step(now, now + KT * S::ROWB, cached, (tile0 + t) * KT, src.ctx, s_up, sc);
-    if (t + 2 < n_tiles) place(t + 2);
+  __device__ __forceinline__ Places places(const Segment& s, int base) const {
+    const int lane = threadIdx.x & 63, key = (s.tile0 + base + lane) * KT + (int)(threadIdx.x >> 6) * RW;
+    Places r = {-1, base};
+    if (p.one_place && key + RW <= s.ctx && base + lane < s.n_tiles) {
+      const int b = key / p.block_size, x = p.block_table[(int64_t)s.q * p.max_blocks + b];
+      if (x >= 0 && x < p.n_blocks) r.at = x * p.block + (key - b * p.block_size) * p.slot;
+    }
+    return r;
+  }
+  static __device__ __forceinline__ int64_t place_of(const Places& f, int t) {
+    const int lane = t - f.base;
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(f.at >> 32), lane) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)f.at, lane));
   }
 
-  __device__ __forceinline__ void run(lds_u8* b0, lds_u8* b1) {
-    if (n_tiles <= 0) return;
-    place(0);
-    copy(b0, 0);
-    if (n_tiles > 1) place(1);
-    for (int t = 0; t < n_tiles; t += 2) {
-      turn(b0, b1, t);
-      if (t + 1 < n_tiles) turn(b1, b0, t + 1);
+  __device__ __forceinline__ Rows rows_of(const Segment& s, int t) const {
+    const int tid = opaque_tid(), key = (s.tile0 + t) * KT + (tid >> 6) * RW + (tid & 63) % RW;
+    // what is not a key is read from row 0, which every row sees: with a weight of zero it adds nothing
+    uint64_t a = reinterpret_cast<uint64_t>(s.k_rows) | 1;
+    bool ok = false;
+    if (key < s.ctx) {
+      const int b = key / p.block_size, x = p.block_table[(int64_t)s.q * p.max_blocks + b];
+      if (x >= 0 && x < p.n_blocks) {
+        a = reinterpret_cast<uint64_t>(s.k_cache + x * p.block + (key - b * p.block_size) * p.slot);
+        ok = true;
+      }
+    } else if (key < s.keys) {
+      a = reinterpret_cast<uint64_t>(s.k_rows + (int64_t)(key - s.ctx) * p.new_row) | 1;
+    }
+    return {a, (uint32_t)__ballot(ok) & ((1u << RW) - 1)};
+  }
+
+  // what copying tile t will need; called for the tiles of a segment one after the other
+  __device__ __forceinline__ void prepare(const Segment& s, int t, Places& f, Rows& r) const {
+    if (t - f.base == 64) f = places(s, t);
+    if (place_of(f, t) < 0) r = rows_of(s, t);
+  }
+
+  __device__ __forceinline__ static void copy16(const uint8_t* from, lds_u8* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  }
+  // a lane's 16 bytes land at its place in the instruction's 1 KiB: the words of a row are permuted where they are read
+  __device__ __forceinline__ void copy(const Segment& s, int t, const Places& f, const Rows& r, lds_u8* to, uint32_t* valid) const {
+    const int tid = opaque_tid(), lane = tid & 63, wave = uniform(tid >> 6);
+    lds_u8* at = to + wave * RW * S::ROWB;
+    const int64_t place = place_of(f, t);
+    if (place >= 0) {
+      if (lane == 0) valid[wave] = (1u << RW) - 1;
+      const uint8_t *k = s.k_cache + place, *v = k + to_v_cache;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        copy16(k + offset[j], at + j * RPI * S::ROWB);
+        copy16(v + offset[j], at + (KT + j * RPI) * S::ROWB);
+      }
+      return;
+    }
+    if (lane == 0) valid[wave] = r.valid;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int row = j * RPI + lane / S::CH, word = (lane % S::CH) ^ ((wave * RW + row) & S::SWZ);
+      const uint64_t x = __shfl((unsigned long long)r.at, row);
+      const uint8_t* k = reinterpret_cast<const uint8_t*>(x & ~1ull) + min(word, last_word) * 16;
+      copy16(k, at + j * RPI * S::ROWB);
+      copy16(k + (x & 1 ? to_v_rows : to_v_cache), at + (KT + j * RPI) * S::ROWB);
     }
   }
 };
 
-template <bool BF16, int DP, int MQ, int WK, int KT>
+template <bool BF16, int DP, int MQ, int WK>
 __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 ? 2 : 1) void attention_kernel(AttentionJob p, AttentionSpace ws) {
-  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
-  typedef AttentionTile<BF16, DP, MQ, WK, KT> Tile;
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
+  typedef AttentionTile<BF16, DP, MQ, WK> Tile;
+  typedef TileCopy<BF16, DP, MQ, WK> Copy;
   constexpr int ESZ = S::ESZ, BM = S::BM;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + S::LDS);   // [M + 1]: row of a row's parent
   __shared__ uint32_t s_valid[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
   const int wq = wave / WK, wk = wave % WK;
@@ -347,7 +390,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   // ---- this workgroup's tiles: an equal share of all, in the order sequence, head, block, tile ----
   uint64_t all = 0;
   for (int q0 = 0; q0 < p.batch; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles<KT>(p, q0 + lane, BM).total : 0;
+    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM).total : 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
     all += t;
@@ -365,7 +408,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   int q = 0;
   uint64_t start = 0;   // of sequence q
   for (int q0 = 0;; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles<KT>(p, q0 + lane, BM).total : 0, sum = t;
+    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM).total : 0, sum = t;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const uint64_t y = __shfl_up((unsigned long long)sum, d);
@@ -381,43 +424,75 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     start = uniform(start + (uint64_t)__shfl((unsigned long long)sum, 63));
   }
   Owner mine = {-1, 0, 0, 0};
-  SeqTiles sq = seq_tiles<KT, true>(p, q, BM);
-  // the first segment's place; the others start at the next unit's first tile
-  uint64_t unit = uniform((at - start) / (uint64_t)sq.tiles);
-  int tile0 = uniform((int)(at - start - unit * (uint64_t)sq.tiles));
-  int g = uniform((int)(unit / (uint64_t)sq.blocks)), block = uniform((int)(unit - (uint64_t)g * (uint64_t)sq.blocks));
+
+  // ---- segments ----
+  auto finish = [&](Segment& s, uint64_t from) {   // the rest of a segment from its unit and first tile, which is tile `from` of all
+    s.n_seg = (int)min(end - from, (uint64_t)(s.tiles - s.tile0));
+    s.keys = s.ctx + min(s.nodes, (s.block * BM + BM - 1) / G) + 1;
+    s.n_tiles = max(min(s.n_seg, (s.keys + KT - 1) / KT - s.tile0), 1);   // (tiles behind that hold rows that are nobody's ancestor)
+    s.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)s.g * p.cache_head;
+    s.k_rows = static_cast<const uint8_t*>(p.k_new) + s.q * p.new_seq + (int64_t)s.g * p.new_head;
+  };
+  auto of_sequence = [&](Segment& s, int seq) {
+    const SeqTiles t = seq_tiles<true>(p, seq, BM);
+    s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
+    return t.total;
+  };
+  auto following = [&](const Segment& s, uint64_t from) {   // the segment behind s; there is one
+    Segment n = s;
+    n.tile0 = 0;
+    if (++n.block == n.blocks) {
+      n.block = 0;
+      if (++n.g == p.kv_heads) {
+        n.g = 0;
+        do ++n.q;
+        while (of_sequence(n, n.q) == 0);
+      }
+    }
+    finish(n, from);
+    return n;
+  };
+  Segment now;
+  of_sequence(now, q);
+  {
+    const uint64_t unit = uniform((at - start) / (uint64_t)now.tiles);
+    now.tile0 = uniform((int)(at - start - unit * (uint64_t)now.tiles));
+    now.g = uniform((int)(unit / (uint64_t)now.blocks));
+    now.block = uniform((int)(unit - (uint64_t)now.g * (uint64_t)now.blocks));
+    finish(now, at);
+  }
 
   // a negative scale goes into the queries' sign, a scale of zero makes them zero: the largest product has the largest weight
   const float q_sign = p.scale < 0 ? -1.0f : p.scale == 0 ? 0.0f : 1.0f;
   const float sc = (p.scale == 0 ? 1.0f : fabsf(p.scale)) * kLog2e;
   const int last_word = p.head_dim * ESZ / 16 - 1;
 
-  while (at < end) {
-    const int n_seg = (int)min(end - at, (uint64_t)(sq.tiles - tile0));
-    const int rows = (sq.nodes + 1) * G - block * BM;                          // query rows from this unit's first on
-    const int last_row = min(sq.nodes, (block * BM + BM - 1) / G);             // its last tree row
-    KeySource src;
-    src.ctx = sq.ctx;
-    src.keys = sq.ctx + last_row + 1;                                          // what it sees at most
-    src.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)g * p.cache_head;
-    src.k_rows = static_cast<const uint8_t*>(p.k_new) + q * p.new_seq + (int64_t)g * p.new_head;
-    src.to_v_cache = static_cast<const uint8_t*>(p.v) - static_cast<const uint8_t*>(p.k);
-    src.to_v_rows = static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new);
-    src.table = p.block_table + (int64_t)q * p.max_blocks;
-    src.last_word = last_word;
-    const int n_tiles = min(n_seg, (src.keys + KT - 1) / KT - tile0);          // (tiles behind that: rows that are nobody's ancestor)
-    __syncthreads();   // the last unit is done with the memory
-    if ((tile0 + n_tiles) * KT > sq.ctx)
-      for (int i = tid; i < last_row; i += 256) {
-        const int up = p.node_parent[(int64_t)q * p.M + i];
+  Copy copy = {p, s_valid, last_word, static_cast<const uint8_t*>(p.v) - static_cast<const uint8_t*>(p.k),
+               static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new)};
+  copy.init();
+  typename Copy::Places f = copy.places(now, 0), f_next = {-1, 0};
+  typename Copy::Rows r = {0, 0}, r_next = {0, 0};
+  copy.prepare(now, 0, f, r);
+  copy.copy(now, 0, f, r, (lds_u8*)smem, s_valid[0]);
+  int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
+  Segment next = now;
+  for (bool more = true; more;) {
+    more = at + now.n_seg < end;
+    const int rows = (now.nodes + 1) * G - now.block * BM;                     // query rows from this unit's first on
+    // ---- parents' rows, where tiles hold rows (two sets: others may still be at the last segment) ----
+    uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + S::LDS) + (n_units & 1) * ((p.M + 8) & ~7);
+    if ((now.tile0 + now.n_tiles) * KT > now.ctx)
+      for (int i = tid; i < now.keys - now.ctx - 1; i += 256) {
+        const int up = p.node_parent[(int64_t)now.q * p.M + i];
         s_up[i + 1] = (uint16_t)(up >= 0 && up < i ? up + 1 : 0);
       }
+    // ---- queries ----
     Tile x;
 #pragma unroll
     for (int mq = 0; mq < MQ; ++mq) {
-      const int m = (wq * MQ + mq) * 16 + l16, mm = m < rows ? block * BM + m : 0;
+      const int m = (wq * MQ + mq) * 16 + l16, mm = m < rows ? now.block * BM + m : 0;
       x.row_of[mq] = mm / G;
-      const uint8_t* from = static_cast<const uint8_t*>(p.q) + q * p.q_seq + (int64_t)x.row_of[mq] * p.q_row + (int64_t)(g * G + mm % G) * p.q_head;
+      const uint8_t* from = static_cast<const uint8_t*>(p.q) + now.q * p.q_seq + (int64_t)x.row_of[mq] * p.q_row + (int64_t)(now.g * G + mm % G) * p.q_head;
 #pragma unroll
       for (int s = 0; s < Tile::QS; ++s) {
         const int word = s * 4 + grp;
@@ -434,14 +509,34 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d) x.o[mq][d] = (f32x4){0, 0, 0, 0};
     }
-    AttentionLoop<BF16, DP, MQ, WK, KT> loop = {p, src, x, s_valid, s_up, sc, tile0, n_tiles, 0, 0};
-    loop.run((lds_u8*)smem, (lds_u8*)(smem + S::LDS / 2));
+    if (now.n_tiles > 1) copy.prepare(now, 1, f, r);
+    if (more) {
+      next = following(now, at + now.n_seg);
+      f_next = copy.places(next, 0);
+      copy.prepare(next, 0, f_next, r_next);
+    }
+
+    // ---- tiles.  The next one is copied into the other buffer while one is worked on; the two buffers are distinct objects to
+    // the compiler (restrict), so that a read of one does not wait for the copies into the other ----
+    auto tile = [&](lds_u8* cur, lds_u8* other, int t) {
+      attention_turn<BF16, DP, MQ, WK>(
+          x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, [&](lds_u8* to) {
+            if (t + 1 < now.n_tiles) copy.copy(now, t + 1, f, r, to, s_valid[(turn + 1) & 1]);
+            else if (more) copy.copy(next, 0, f_next, r_next, to, s_valid[(turn + 1) & 1]);
+          });
+      if (t + 2 < now.n_tiles) copy.prepare(now, t + 2, f, r);
+      ++turn;
+    };
+    for (int t = 0; t < now.n_tiles;) {
+      if (turn & 1) tile((lds_u8*)(smem + S::LDS / 2), (lds_u8*)smem, t++);
+      if (t < now.n_tiles && !(turn & 1)) tile((lds_u8*)smem, (lds_u8*)(smem + S::LDS / 2), t++);
+    }
 #pragma unroll
     for (int mq = 0; mq < MQ; ++mq) x.l_run[mq] = groups_sum(x.l_run[mq]);
 
-    // ---- join of the waves that took other keys of the same rows ----
+    // ---- join of the waves that took other keys of the same rows, through the buffer of the last tile ----
     if constexpr (WK > 1) {
-      float* box = reinterpret_cast<float*>(smem);
+      float* box = reinterpret_cast<float*>(smem + ((turn - 1) & 1) * (S::LDS / 2));
       constexpr int PER = MQ * (DP / 4 + 2);   // values per lane
       __syncthreads();
       if (wk > 0) {
@@ -476,9 +571,9 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     }
 
     // ---- out, or what has been summed so far ----
-    const bool whole = n_seg == sq.tiles;
-    if (!whole && tile0 == 0)   // the unit ends in the workgroup that takes its last tile
-      mine = {q, g, block, (int)(((at + (uint64_t)sq.tiles) * groups - 1) / all)};
+    const bool whole = now.n_seg == now.tiles;
+    if (!whole && now.tile0 == 0)   // the unit ends in the workgroup that takes its last tile
+      mine = {now.q, now.g, now.block, (int)(((at + (uint64_t)now.tiles) * groups - 1) / all)};
     if (wk == 0) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
@@ -486,7 +581,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         if (m < rows) {
           if (whole) {
             const float inv = 1.0f / x.l_run[mq];
-            uint8_t* to = static_cast<uint8_t*>(p.out) + q * p.out_seq + (int64_t)x.row_of[mq] * p.out_row + (int64_t)(g * G + (block * BM + m) % G) * p.out_head;
+            uint8_t* to = static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)x.row_of[mq] * p.out_row + (int64_t)(now.g * G + (now.block * BM + m) % G) * p.out_head;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
               const int e = d * 16 + grp * 4;
@@ -497,7 +592,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
               }
             }
           } else {
-            float* to = ws.part + ((int64_t)(me * 2 + (tile0 == 0 ? 1 : 0)) * BM + m) * (DP + 4);
+            float* to = ws.part + ((int64_t)(me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + m) * (DP + 4);
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<f32x4*>(to + d * 16 + grp * 4) = x.o[mq][d];
             if (grp == 0) to[DP] = x.m_run[mq], to[DP + 1] = x.l_run[mq];
@@ -505,16 +600,11 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         }
       }
     }
-    at += n_seg;
-    tile0 = 0;
-    if (++block == sq.blocks) {
-      block = 0;
-      if (++g == p.kv_heads && at < end) {
-        g = 0;
-        do sq = seq_tiles<KT, true>(p, ++q, BM);
-        while (sq.total == 0);
-      }
-    }
+    at += now.n_seg;
+    now = next;
+    f = f_next;
+    r = r_next;
+    ++n_units;
   }
   if (tid == 0) ws.owner[me] = mine;
 }
@@ -638,26 +728,26 @@ int64_t attention_workspace(int batch, int M, int q_heads, int kv_heads, int hea
   return (int64_t)a.groups * sizeof(Owner) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
 }
 
-template <bool BF16, int DP, int MQ, int WK, int KT>
+template <bool BF16, int DP, int MQ, int WK>
 static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
-  typedef AttentionShape<BF16, DP, MQ, WK, KT> S;
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
   AttentionSpace ws;
   ws.owner = static_cast<Owner*>(job.workspace);
   ws.part = reinterpret_cast<float*>(ws.owner + plan.groups);
   ws.groups = plan.groups;
   ws.least = plan.least;
-  const size_t smem = S::LDS + (((size_t)job.M + 1) * 2 + 15) / 16 * 16;
+  const size_t smem = S::LDS + 2 * (((size_t)job.M + 8) & ~(size_t)7) * sizeof(uint16_t);
   int device = 0;
   hipError_t e = hipGetDevice(&device);
   if (e != hipSuccess) return e;
   static std::atomic<uint64_t> allowed{0};   // devices where this kernel may have so much memory, per instantiation
   if (device >= 64 || !((allowed.load(std::memory_order_relaxed) >> device) & 1)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<BF16, DP, MQ, WK, KT>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            S::LDS + (kMaxTreeItems + 1 + 7) / 8 * 16);
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<BF16, DP, MQ, WK>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            S::LDS + 2 * ((kMaxTreeItems + 8) & ~7) * (int)sizeof(uint16_t));
     if (e != hipSuccess) return e;
     if (device < 64) allowed.fetch_or(1ull << device, std::memory_order_relaxed);
   }
-  hipLaunchKernelGGL((attention_kernel<BF16, DP, MQ, WK, KT>), dim3(plan.groups), dim3(256), smem, st, job, ws);
+  hipLaunchKernelGGL((attention_kernel<BF16, DP, MQ, WK>), dim3(plan.groups), dim3(256), smem, st, job, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attention_join_kernel<BF16, DP, S::BM>), dim3(plan.groups, S::BM / 16), dim3(256), 0, st, job, ws);
@@ -670,25 +760,25 @@ hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st) 
     hipLaunchKernelGGL(attention_f32_kernel, dim3(job.M + 1, job.q_heads, job.batch), dim3(256), 0, st, job);
     return hipGetLastError();
   }
-#define LAUNCH(BF16, DP, BM, MQ, WK, KT) \
-  if (bf16 == BF16 && a.dp == DP && a.bm == BM) return launch_attention_t<BF16, DP, MQ, WK, KT>(job, a, st)
-  LAUNCH(true, 64, 16, 1, 4, 64);
-  LAUNCH(true, 64, 32, 1, 2, 64);
-  LAUNCH(true, 64, 64, 1, 1, 64);
-  LAUNCH(true, 64, 128, 2, 1, 64);
-  LAUNCH(true, 128, 16, 1, 4, 64);
-  LAUNCH(true, 128, 32, 1, 2, 64);
-  LAUNCH(true, 128, 64, 1, 1, 64);
-  LAUNCH(true, 128, 128, 2, 1, 64);
-  LAUNCH(true, 256, 16, 1, 4, 64);
-  LAUNCH(true, 256, 32, 1, 2, 64);
-  LAUNCH(true, 256, 64, 1, 1, 64);
-  LAUNCH(false, 64, 16, 1, 4, 64);
-  LAUNCH(false, 64, 32, 1, 2, 64);
-  LAUNCH(false, 64, 64, 1, 1, 64);
-  LAUNCH(false, 128, 16, 1, 4, 64);
-  LAUNCH(false, 128, 32, 1, 2, 64);
-  LAUNCH(false, 128, 64, 1, 1, 64);
+#define LAUNCH(BF16, DP, BM, MQ, WK) \
+  if (bf16 == BF16 && a.dp == DP && a.bm == BM) return launch_attention_t<BF16, DP, MQ, WK>(job, a, st)
+  LAUNCH(true, 64, 16, 1, 4);
+  LAUNCH(true, 64, 32, 1, 2);
+  LAUNCH(true, 64, 64, 1, 1);
+  LAUNCH(true, 64, 128, 2, 1);
+  LAUNCH(true, 128, 16, 1, 4);
+  LAUNCH(true, 128, 32, 1, 2);
+  LAUNCH(true, 128, 64, 1, 1);
+  LAUNCH(true, 128, 128, 2, 1);
+  LAUNCH(true, 256, 16, 1, 4);
+  LAUNCH(true, 256, 32, 1, 2);
+  LAUNCH(true, 256, 64, 1, 1);
+  LAUNCH(false, 64, 16, 1, 4);
+  LAUNCH(false, 64, 32, 1, 2);
+  LAUNCH(false, 64, 64, 1, 1);
+  LAUNCH(false, 128, 16, 1, 4);
+  LAUNCH(false, 128, 32, 1, 2);
+  LAUNCH(false, 128, 64, 1, 1);
 #undef LAUNCH
   return hipErrorInvalidValue;
 }

@@ -84,6 +84,7 @@ extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_ro
   j.block_table = block_table, j.ctx_len = ctx_len, j.node_parent = node_parent, j.n_nodes = n_nodes;
   j.batch = batch, j.M = M, j.q_heads = q_heads, j.kv_heads = kv_heads, j.head_dim = head_dim;
   j.max_blocks = max_blocks, j.n_blocks = cache->n_blocks, j.block_size = cache->block_size;
+  j.one_place = cache->block_size % 16 == 0 && j.slot >= 0 && j.slot < (1 << 26);
   j.scale = scale, j.workspace = workspace;
   HIP_TRY(launch_attention(j, dtype == SPEC_BF16, static_cast<hipStream_t>(hip_stream)));
   return SPEC_OK;
