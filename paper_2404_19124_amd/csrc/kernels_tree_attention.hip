@@ -49,21 +49,33 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
-// A sequence's share of the tiles.
+// words that nobody writes while the kernel runs, at addresses that are the same in every lane: scalar loads
+typedef const __attribute__((address_space(4))) int32_t* scalar_i32;
+
+// The work is cut into equal shares by COST: a unit costs its tiles and kUnitCost more for its queries and results (a sequence
+// with nothing cached, 24 units of one tile in one share: that workgroup took a third longer than all others).
+constexpr int kUnitCost = 1;
+
 struct SeqTiles {
   int ctx, nodes, tiles, blocks;   // cached tokens, last row, tiles per unit, units per key/value head
-  uint64_t total;                  // tiles of all units
+  uint64_t total;                  // cost of all units
 };
 template <bool UNIFORM = false>
 __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int BM) {
   SeqTiles s;
-  int ctx = p.ctx_len[q], nodes = p.n_nodes ? p.n_nodes[q] : p.M;
-  if (UNIFORM) ctx = uniform(ctx), nodes = uniform(nodes);
+  int ctx, nodes;
+  if (UNIFORM) {
+    ctx = *(scalar_i32)(p.ctx_len + q);
+    nodes = p.n_nodes ? *(scalar_i32)(p.n_nodes + q) : p.M;
+  } else {
+    ctx = p.ctx_len[q];
+    nodes = p.n_nodes ? p.n_nodes[q] : p.M;
+  }
   s.ctx = min(max(ctx, 0), p.max_blocks * p.block_size);
   s.nodes = min(max(nodes, -1), p.M);
   s.tiles = (s.ctx + s.nodes + KT) / KT;
   s.blocks = (int)(((int64_t)(s.nodes + 1) * (p.q_heads / p.kv_heads) + BM - 1) / BM);
-  s.total = (uint64_t)s.tiles * (uint64_t)s.blocks * (uint64_t)p.kv_heads;
+  s.total = (uint64_t)(s.tiles + kUnitCost) * (uint64_t)s.blocks * (uint64_t)p.kv_heads;
   return s;
 }
 
@@ -77,7 +89,7 @@ struct AttentionSpace {
   float* part;      // [groups][2][BM][DP + 4]: o, m, l of the segment that goes on from an earlier workgroup, of the one that
                     // goes on to a later one
   int groups;       // workgroups of the launch
-  int least;        // tiles that a workgroup takes at least
+  int least;        // cost that a workgroup takes at least
 };
 
 // two buffers of keys and values
@@ -264,6 +276,7 @@ __device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& 
 struct Segment {
   int q, g, block;                   // sequence, key/value head, block of BM query rows
   int ctx, nodes, tiles, blocks;     // as SeqTiles
+  int heads, last_head;              // heads of a group, and the last one of this group: see below
   int tile0, n_seg, n_tiles;         // first tile, tiles, and those of them that hold keys of its rows (at least one)
   int keys;                          // cached tokens and rows up to its last one
   const uint8_t *k_cache, *k_rows;   // of the head
@@ -387,7 +400,11 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   const int wq = wave / WK, wk = wave % WK;
   const int G = p.q_heads / p.kv_heads;
 
-  // ---- this workgroup's tiles: an equal share of all, in the order sequence, head, block, tile ----
+  // ---- this workgroup's tiles: an equal share of all, in the order sequence, group of heads, block, head, tile.  A group has as
+  // many heads as a share holds units: the blocks of a head, which read the same keys, then run beside each other on one XCD
+  // (consecutive shares do) and not one after the other in one workgroup.  Batch of 32, 8 key/value heads of 128, 384 query rows
+  // a head in three blocks: 298 us with all tiles of a block before the next one's (940 MB from beyond the L2 for 385 MB of keys
+  // and values) and no unit cost, 244 us so ----
   uint64_t all = 0;
   for (int q0 = 0; q0 < p.batch; q0 += 64) {
     uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM).total : 0;
@@ -395,7 +412,6 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
     all += t;
   }
-  // (consecutive shares, which meet in the same keys, run on the same XCD)
   const int me = (int)(blockIdx.x % 8) * (ws.groups / 8) + (int)(blockIdx.x / 8);
   all = uniform(all);
   const uint64_t groups = min((uint64_t)ws.groups, (all + ws.least - 1) / ws.least);
@@ -405,6 +421,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   }
   uint64_t at = uniform(all * me / groups);
   const uint64_t end = uniform(all * (me + 1) / groups);
+  const int share = uniform((int)min(all / groups, (uint64_t)(1 << 30)));
   int q = 0;
   uint64_t start = 0;   // of sequence q
   for (int q0 = 0;; q0 += 64) {
@@ -426,40 +443,61 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   Owner mine = {-1, 0, 0, 0};
 
   // ---- segments ----
-  auto finish = [&](Segment& s, uint64_t from) {   // the rest of a segment from its unit and first tile, which is tile `from` of all
-    s.n_seg = (int)min(end - from, (uint64_t)(s.tiles - s.tile0));
+  auto of_sequence = [&](Segment& s, int seq) {
+    const SeqTiles t = seq_tiles<true>(p, seq, BM);
+    s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
+    s.heads = uniform(min(max(share / (t.tiles + kUnitCost), 1), p.kv_heads));
+    return t.total;
+  };
+  // the rest of a segment, `cost` of whose unit other workgroups bear, from place `from` on; false: there is no tile in it
+  auto finish = [&](Segment& s, uint64_t from, int cost) {
+    const int upto = cost + (int)min(end - from, (uint64_t)(s.tiles + kUnitCost - cost));
+    s.tile0 = max(cost - kUnitCost, 0);
+    s.n_seg = max(upto - kUnitCost, 0) - s.tile0;
     s.keys = s.ctx + min(s.nodes, (s.block * BM + BM - 1) / G) + 1;
     s.n_tiles = max(min(s.n_seg, (s.keys + KT - 1) / KT - s.tile0), 1);   // (tiles behind that hold rows that are nobody's ancestor)
     s.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)s.g * p.cache_head;
     s.k_rows = static_cast<const uint8_t*>(p.k_new) + s.q * p.new_seq + (int64_t)s.g * p.new_head;
+    return s.n_seg > 0;
   };
-  auto of_sequence = [&](Segment& s, int seq) {
-    const SeqTiles t = seq_tiles<true>(p, seq, BM);
-    s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
-    return t.total;
-  };
-  auto following = [&](const Segment& s, uint64_t from) {   // the segment behind s; there is one
-    Segment n = s;
-    n.tile0 = 0;
-    if (++n.block == n.blocks) {
-      n.block = 0;
-      if (++n.g == p.kv_heads) {
-        n.g = 0;
-        do ++n.q;
-        while (of_sequence(n, n.q) == 0);
+  // the segment behind s, whose unit starts at place `from`; false: there is none
+  auto following = [&](Segment& s, uint64_t from) {
+    if (from >= end) return false;
+    if (s.g < s.last_head) {
+      ++s.g;
+    } else if (++s.block < s.blocks) {
+      s.g -= (s.g % s.heads);   // (groups start at multiples of their size)
+    } else {
+      s.block = 0;
+      if (++s.g == p.kv_heads) {
+        s.g = 0;
+        do ++s.q;
+        while (of_sequence(s, s.q) == 0);
       }
+      s.last_head = min(s.g + s.heads, p.kv_heads) - 1;
     }
-    finish(n, from);
-    return n;
+    return finish(s, from, 0);
   };
   Segment now;
   of_sequence(now, q);
+  uint64_t unit_end;   // of the segment that is worked on
+  bool more;
   {
-    const uint64_t unit = uniform((at - start) / (uint64_t)now.tiles);
-    now.tile0 = uniform((int)(at - start - unit * (uint64_t)now.tiles));
-    now.g = uniform((int)(unit / (uint64_t)now.blocks));
-    now.block = uniform((int)(unit - (uint64_t)now.g * (uint64_t)now.blocks));
-    finish(now, at);
+    const int span = now.tiles + kUnitCost;
+    const uint64_t unit = uniform((at - start) / (uint64_t)span);
+    const int cost = uniform((int)(at - start - unit * (uint64_t)span));
+    const int per = now.heads * now.blocks, group = uniform((int)(unit / (uint64_t)per)), in = uniform((int)(unit - (uint64_t)group * (uint64_t)per));
+    now.last_head = min((group + 1) * now.heads, p.kv_heads) - 1;
+    const int size = now.last_head + 1 - group * now.heads;
+    now.block = uniform(in / size);
+    now.g = uniform(group * now.heads + in - now.block * size);
+    unit_end = at + (uint64_t)(span - cost);
+    more = finish(now, at, cost);
+    if (!more && (more = following(now, unit_end))) unit_end += (uint64_t)(now.tiles + kUnitCost);   // (nothing but the cost of its queries)
+  }
+  if (!more) {
+    if (tid == 0) ws.owner[me] = mine;
+    return;
   }
 
   // a negative scale goes into the queries' sign, a scale of zero makes them zero: the largest product has the largest weight
@@ -475,9 +513,9 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   copy.prepare(now, 0, f, r);
   copy.copy(now, 0, f, r, (lds_u8*)smem, s_valid[0]);
   int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
-  Segment next = now;
-  for (bool more = true; more;) {
-    more = at + now.n_seg < end;
+  while (more) {
+    Segment next = now;
+    more = following(next, unit_end);
     const int rows = (now.nodes + 1) * G - now.block * BM;                     // query rows from this unit's first on
     // ---- parents' rows, where tiles hold rows (two sets: others may still be at the last segment) ----
     uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + S::LDS) + (n_units & 1) * ((p.M + 8) & ~7);
@@ -511,7 +549,6 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     }
     if (now.n_tiles > 1) copy.prepare(now, 1, f, r);
     if (more) {
-      next = following(now, at + now.n_seg);
       f_next = copy.places(next, 0);
       copy.prepare(next, 0, f_next, r_next);
     }
@@ -573,7 +610,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     // ---- out, or what has been summed so far ----
     const bool whole = now.n_seg == now.tiles;
     if (!whole && now.tile0 == 0)   // the unit ends in the workgroup that takes its last tile
-      mine = {now.q, now.g, now.block, (int)(((at + (uint64_t)now.tiles) * groups - 1) / all)};
+      mine = {now.q, now.g, now.block, (int)((unit_end * groups - 1) / all)};
     if (wk == 0) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
@@ -600,7 +637,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         }
       }
     }
-    at += now.n_seg;
+    unit_end += (uint64_t)(next.tiles + kUnitCost);
     now = next;
     f = f_next;
     r = r_next;
