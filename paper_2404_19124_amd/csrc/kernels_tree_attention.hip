@@ -15,6 +15,7 @@
 
 namespace specdraft {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -82,6 +83,7 @@ __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int 
 // What a workgroup that ends inside a unit leaves: see the join below.
 struct Owner {
   int q, g, block, last;   // the unit that starts in this workgroup and ends in workgroup `last`; q < 0: none
+  int rows;                // its query rows
 };
 
 struct AttentionSpace {
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     }
     start = uniform(start + (uint64_t)__shfl((unsigned long long)sum, 63));
   }
-  Owner mine = {-1, 0, 0, 0};
+  Owner mine = {-1, 0, 0, 0, 0};
 
   // ---- segments ----
   auto of_sequence = [&](Segment& s, int seq) {
@@ -610,7 +612,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     // ---- out, or what has been summed so far ----
     const bool whole = now.n_seg == now.tiles;
     if (!whole && now.tile0 == 0)   // the unit ends in the workgroup that takes its last tile
-      mine = {now.q, now.g, now.block, (int)((unit_end * groups - 1) / all)};
+      mine = {now.q, now.g, now.block, (int)((unit_end * groups - 1) / all), min(rows, BM)};
     if (wk == 0) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
@@ -646,34 +648,44 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   if (tid == 0) ws.owner[me] = mine;
 }
 
-// Units that several workgroups took part in: workgroup (w, y) joins 16 query rows of the one that started in workgroup w of
-// the launch above, in the order of the keys.
+// Units that several workgroups took part in: workgroup (w, y) joins some query rows of the one that started in workgroup w of
+// the launch above, in the order of the keys.  One small call (32 heads of 58 query rows, 12 parts each) reads and writes as
+// much for its parts as for its keys and values: the rows are spread over as many workgroups as there are.
+constexpr int join_rows(int DP) { return 256 / (DP / 4); }
 template <bool BF16, int DP, int BM>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, AttentionSpace ws) {
   const int w = blockIdx.x, tid = threadIdx.x, G = p.q_heads / p.kv_heads;
   const Owner u = ws.owner[w];
-  if (u.q < 0) return;
-  const int nodes = p.n_nodes ? min(max(p.n_nodes[u.q], -1), p.M) : p.M;
   constexpr int PER = DP / 4;   // threads of a row
-  for (int i = tid; i < 16 * PER; i += 256) {
-    const int m = blockIdx.y * 16 + i / PER, e = i % PER * 4, mm = u.block * BM + m;
-    if (mm >= (nodes + 1) * G || e >= p.head_dim) continue;
-    f32x4 o = {0, 0, 0, 0};
-    float top = kLowest, l = 0;
-    for (int x = w; x <= u.last; ++x) {
+  const int m = blockIdx.y * join_rows(DP) + tid / PER, e = tid % PER * 4, mm = u.block * BM + m;
+  if (u.q < 0 || m >= u.rows || e >= p.head_dim) return;
+  f32x4 o = {0, 0, 0, 0};
+  float top = kLowest, l = 0;
+  // eight parts' loads at a time: one after the other they wait for each other's latency
+  for (int x0 = w; x0 <= u.last; x0 += 8) {
+    f32x4 po[8];
+    f32x2 pm[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int x = min(x0 + j, u.last);
       const float* from = ws.part + ((int64_t)(x * 2 + (x == w ? 1 : 0)) * BM + m) * (DP + 4);
-      const f32x4 po = *reinterpret_cast<const f32x4*>(from + e);
-      const float pm = from[DP], m_new = fmaxf(top, pm), keep = __builtin_amdgcn_exp2f(top - m_new), add = __builtin_amdgcn_exp2f(pm - m_new);
-      o = o * keep + po * add;
-      l = l * keep + from[DP + 1] * add;
+      po[j] = *reinterpret_cast<const f32x4*>(from + e);
+      pm[j] = *reinterpret_cast<const f32x2*>(from + DP);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (x0 + j > u.last) break;
+      const float m_new = fmaxf(top, pm[j][0]), keep = __builtin_amdgcn_exp2f(top - m_new), add = __builtin_amdgcn_exp2f(pm[j][0] - m_new);
+      o = o * keep + po[j] * add;
+      l = l * keep + pm[j][1] * add;
       top = m_new;
     }
-    const float inv = 1.0f / l;
-    o = o * inv;
-    uint8_t* to = static_cast<uint8_t*>(p.out) + u.q * p.out_seq + (int64_t)(mm / G) * p.out_row + (int64_t)(u.g * G + mm % G) * p.out_head;
-    if constexpr (BF16) *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(o[2], o[3]) << 32 | f32_to_bf16_pair(o[0], o[1]);
-    else *reinterpret_cast<f32x4*>(to + e * 4) = o;
   }
+  const float inv = 1.0f / l;
+  o = o * inv;
+  uint8_t* to = static_cast<uint8_t*>(p.out) + u.q * p.out_seq + (int64_t)(mm / G) * p.out_row + (int64_t)(u.g * G + mm % G) * p.out_head;
+  if constexpr (BF16) *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(o[2], o[3]) << 32 | f32_to_bf16_pair(o[0], o[1]);
+  else *reinterpret_cast<f32x4*>(to + e * 4) = o;
 }
 
 // float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): one workgroup per
@@ -787,7 +799,7 @@ static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPla
   hipLaunchKernelGGL((attention_kernel<BF16, DP, MQ, WK>), dim3(plan.groups), dim3(256), smem, st, job, ws);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attention_join_kernel<BF16, DP, S::BM>), dim3(plan.groups, S::BM / 16), dim3(256), 0, st, job, ws);
+  hipLaunchKernelGGL((attention_join_kernel<BF16, DP, S::BM>), dim3(plan.groups, (S::BM + join_rows(DP) - 1) / join_rows(DP)), dim3(256), 0, st, job, ws);
   return hipGetLastError();
 }
 
