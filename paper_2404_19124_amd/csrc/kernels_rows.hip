@@ -11,8 +11,8 @@
 
 namespace specdraft {
 
-constexpr int kRowThreads = 512;
-constexpr int kRowChunks = 4;   // chunks of 8 tokens that a thread has in flight
+constexpr int row_chunks(bool out) { return out ? 1 : 2; }   // chunks of 8 tokens that a thread has in flight
+constexpr int kWideRows = 512;   // rows of which two fit a CU: 1024 threads each (46 rows of 32000: 12.7 us, with 512: 15.4 us)
 
 // eight neighbours; rows of an odd length start anywhere, so their words are not aligned to 16 bytes (the compiler's memcpy is one
 // 16-byte load all the same)
@@ -23,6 +23,9 @@ __device__ __forceinline__ T load_words(const void* from) {
   return x;
 }
 
+__device__ __forceinline__ float to_f32(uint16_t x) { return bf16_bits_to_f32(x); }
+__device__ __forceinline__ float to_f32(float x) { return x; }
+
 // What changes one sequence's logits (row by row: allowed).
 struct RowPenalty {
   const int32_t* counts;
@@ -31,60 +34,91 @@ struct RowPenalty {
   float rep, pres, freq;
 };
 
-// A token that was seen, or is on the path, by the whole formula; c: its occurrences.
-__device__ __forceinline__ float penalized(float v, int i, int c, bool bit, const RowPenalty& pen) {
+// A token by the whole formula; c: its occurrences.
+__device__ __forceinline__ float penalized(float v, int c, bool bit, float bias, bool allowed, const RowPenalty& pen) {
 // (a product and a difference are rounded one by one: what is chosen must not hang on the compiler's choice)
 #pragma clang fp contract(off)
   if (bit || c > 0) v = v > 0.0f ? v / pen.rep : v * pen.rep;
   v = v - pen.freq * (float)c;
   if (c > 0) v = v - pen.pres;
-  if (pen.bias) v = v + pen.bias[i];
-  if (pen.allowed && !((pen.allowed[i >> 5] >> (i & 31)) & 1)) v = SPEC_NEG_INF;
-  return v;
+  if (pen.bias) v = v + bias;
+  return allowed ? v : SPEC_NEG_INF;
 }
 
-// One workgroup per row.  Few tokens of a row were seen or are on its path: TOUCHED tokens.  The others only take a bias and a
-// mask, eight at a time; the touched ones are left out there (their logits stay as they are) and done one by one from the bits.
-template <bool BF16, bool OUT>
-__global__ __launch_bounds__(kRowThreads, 4) void logits_kernel(LogitsJob p) {
+// One workgroup per row, or (OUT, few rows) per `span` tokens of a row.  Few tokens of a row were seen or are on its path: TOUCHED
+// tokens, and with them the last V % 8.  The others only take a bias and a mask, eight at a time, all loads of a trip requested a
+// trip ahead.  The touched ones are left out there (their logits stay as they are): every wave lists their chunks, logits and all,
+// and works 64 of them off at a time.  Consecutive rows run on one XCD, in whose L2 their sequence's counts stay, and the logits
+// go past it: 2000 counts lie in half of a row's lines.
+// Bound by reading the logits: 32 sequences of 46 rows of 128256 bf16 logits, 2000 tokens emitted, 379 MB in 116 us (3.3 TB/s;
+// torch's largest sum reads 4.0 TB/s).  One element after the other: 603 us; touched tokens gathered again at a row's end: 140 us;
+// rows dealt out over the XCDs one by one: 144 us.
+template <bool BF16, bool OUT, int NT>
+__global__ __launch_bounds__(NT, 4) void logits_kernel(LogitsJob p, int span) {
   typedef uint32_t words __attribute__((ext_vector_type(BF16 ? 4 : 8)));
   typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
   typedef float floatx8 __attribute__((ext_vector_type(8)));
   typedef typename std::conditional<BF16, uint16_t, float>::type T;
-  extern __shared__ int32_t s_node[];   // parents, tokens [M]
+  typedef words loose __attribute__((aligned(sizeof(T))));   // (rows of an odd length start anywhere)
+  constexpr int CHUNKS = row_chunks(OUT), STEP = NT * 8, TRIP = STEP * CHUNKS;
+  constexpr int LIST = 64 * CHUNKS + 64;   // of a wave: a trip adds at most 64 * CHUNKS and finds at most 64 there
+  struct Entry {
+    uint32_t chunk, bits;   // its place in the row, / 8; touched tokens, from bit 8 on those that were seen, from 16 on those that are allowed
+  };
+  union Shared {
+    words raw[NT / 64][LIST];
+    int32_t node[2 * kMaxTreeItems];   // before the list: parents, tokens [M]
+  };
+  __shared__ __attribute__((aligned(32))) Shared s;
+  __shared__ Entry s_list[NT / 64][LIST];
+  auto& s_raw = s.raw;
+  int32_t* s_node = s.node;
   __shared__ float sv[16];
   __shared__ int32_t si[16];
   __shared__ int32_t s_path[kMaxStages];
   __shared__ int s_n;
-  const int R = p.M + 1, q = blockIdx.x / R, r = blockIdx.x - q * R, tid = threadIdx.x, lane = tid & 63, V = p.V;
+  const int R = p.M + 1, me = (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8), q = me / R, r = me - q * R, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = p.V;
+  if (q >= p.batch) return;
   const int nodes = p.n_nodes ? min(max(p.n_nodes[q], -1), p.M) : p.M;
   if (r > nodes) {
-    if (!OUT && tid == 0) p.greedy[blockIdx.x] = -1;
+    if (!OUT && tid == 0) p.greedy[me] = -1;
     return;
   }
-  const T* row = static_cast<const T*>(p.logits) + (int64_t)blockIdx.x * V;
-  T* out = OUT ? static_cast<T*>(p.out) + (int64_t)blockIdx.x * V : nullptr;
-  words x[kRowChunks];
-  auto load = [&](int i0) {
+  const T* row = static_cast<const T*>(p.logits) + (int64_t)me * V;
+  T* out = OUT ? static_cast<T*>(p.out) + (int64_t)me * V : nullptr;
+  const int begin = OUT ? (int)blockIdx.y * span : 0, end = OUT ? min(V, begin + span) : V, full = end & ~7;
+  const int n_words = (V + 31) / 32;
+  RowPenalty pen;
+  pen.counts = p.pen.counts ? p.pen.counts + (int64_t)q * V : nullptr;
+  pen.seen = p.pen.seen ? p.pen.seen + (int64_t)q * n_words : nullptr;
+  const int mask_row = p.pen.allowed ? p.pen.mask_row[me] : -1, bias_row = p.pen.bias ? p.pen.bias_row[q] : -1;
+  pen.bias = bias_row >= 0 && bias_row < p.pen.n_bias ? p.pen.bias + (int64_t)bias_row * V : nullptr;
+  pen.allowed = mask_row >= 0 && mask_row < p.pen.n_allowed ? p.pen.allowed + (int64_t)mask_row * n_words : nullptr;
+  pen.rep = p.pen.repetition ? p.pen.repetition[q] : 1.0f, pen.pres = p.pen.presence ? p.pen.presence[q] : 0.0f;
+  pen.freq = p.pen.frequency ? p.pen.frequency[q] : 0.0f;
+
+  words x[CHUNKS];
+  uint32_t was_seen[CHUNKS] = {}, ok[CHUNKS];
+  auto load = [&](int i0) {   // (lanes behind the last chunk read it again)
 #pragma unroll
-    for (int u = 0; u < kRowChunks; ++u) {
-      const int i = i0 + u * kRowThreads * 8;
-      if (i + 8 <= V) {
-        x[u] = load_words<words>(row + i);
-      } else if (i < V) {   // the row's last tokens
-        T e[8];
+    for (int u = 0; u < CHUNKS; ++u) x[u] = __builtin_nontemporal_load(reinterpret_cast<const loose*>(row + min(i0 + u * STEP, full - 8)));
+    if (pen.seen) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = i + j < V ? row[i + j] : T(0);
-        x[u] = load_words<words>(e);
-      }
+      for (int u = 0; u < CHUNKS; ++u) was_seen[u] = reinterpret_cast<const uint8_t*>(pen.seen)[min(i0 + u * STEP, full - 8) >> 3];
+    }
+#pragma unroll
+    for (int u = 0; u < CHUNKS; ++u) ok[u] = 0xff;
+    if (pen.allowed) {
+#pragma unroll
+      for (int u = 0; u < CHUNKS; ++u) ok[u] = reinterpret_cast<const uint8_t*>(pen.allowed)[min(i0 + u * STEP, full - 8) >> 3];
     }
   };
-  load(tid * 8);
+  if (full > begin) load(begin + tid * 8);
 
   // ---- the tokens on the row's path ----
   int n_path = 0;
   if (p.node_tok && r > 0) {
-    for (int i = tid; i < r; i += kRowThreads) {
+    for (int i = tid; i < r; i += NT) {
       s_node[i] = p.node_parent[(int64_t)q * p.M + i];
       s_node[p.M + i] = p.node_tok[(int64_t)q * p.M + i];
     }
@@ -104,75 +138,104 @@ __global__ __launch_bounds__(kRowThreads, 4) void logits_kernel(LogitsJob p) {
   int path[kMaxStages];   // in scalar registers; -1: none
 #pragma unroll
   for (int j = 0; j < kMaxStages; ++j) path[j] = j < n_path ? __builtin_amdgcn_readfirstlane(s_path[j]) : -1;
-  const int n_words = (V + 31) / 32;
-  RowPenalty pen;
-  pen.counts = p.pen.counts ? p.pen.counts + (int64_t)q * V : nullptr;
-  pen.seen = p.pen.seen ? p.pen.seen + (int64_t)q * n_words : nullptr;
-  pen.rep = p.pen.repetition ? p.pen.repetition[q] : 1.0f, pen.pres = p.pen.presence ? p.pen.presence[q] : 0.0f;
-  pen.freq = p.pen.frequency ? p.pen.frequency[q] : 0.0f;
-  const int bias_row = p.pen.bias ? p.pen.bias_row[q] : -1, mask_row = p.pen.allowed ? p.pen.mask_row[blockIdx.x] : -1;
-  pen.bias = bias_row >= 0 && bias_row < p.pen.n_bias ? p.pen.bias + (int64_t)bias_row * V : nullptr;
-  pen.allowed = mask_row >= 0 && mask_row < p.pen.n_allowed ? p.pen.allowed + (int64_t)mask_row * n_words : nullptr;
 
-  // ---- untouched tokens ----
   float bv = SPEC_NEG_INF;
   int32_t bi = kIdxNone;
-  for (int i0 = tid * 8; i0 - tid * 8 < V; i0 += kRowThreads * 8 * kRowChunks) {
-    uint32_t touched[kRowChunks], ok[kRowChunks];
+  int listed = 0;   // chunks in the wave's list
+  // the last chunks of the list, at most 64
+  auto work_off = [&] {
+    const int n = min(listed, 64);
+    listed -= n;
+    if (lane >= n) return;
+    const Entry e = s_list[wave][listed + lane];
+    for (uint32_t bits = e.bits & 0xff; bits; bits &= bits - 1) {
+      const int j = __builtin_ctz(bits), i = (int)(e.chunk * 8) + j;
+      const bool bit = (e.bits >> (8 + j)) & 1;
+      int c = 0;
+      float bias = 0.0f;
+      if (pen.bias) bias = pen.bias[i];
+      if (pen.counts && (bit || !pen.seen)) c = pen.counts[i];
+      float v = to_f32(reinterpret_cast<const T*>(&s_raw[wave][listed + lane])[j]);
 #pragma unroll
-    for (int u = 0; u < kRowChunks; ++u) {
-      const int i = i0 + u * kRowThreads * 8;
-      touched[u] = 0, ok[u] = 0xff;
-      if (i < V) {
-        // (byte i / 8 of a row of words; a last byte may hold bits behind the row, which `left` takes out)
-        if (pen.seen) touched[u] = reinterpret_cast<const uint8_t*>(pen.seen)[i >> 3];
-        if (pen.allowed) ok[u] = reinterpret_cast<const uint8_t*>(pen.allowed)[i >> 3];
-        if (pen.counts && !pen.seen) {
-          if (i + 8 <= V) {
-            const i32x8 c = load_words<i32x8>(pen.counts + i);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) touched[u] |= c[j] ? 1u << j : 0u;
-          } else {
-            for (int j = 0; i + j < V; ++j) touched[u] |= pen.counts[i + j] ? 1u << j : 0u;
-          }
-        }
+      for (int k = 0; k < kMaxStages; ++k) c += k < n_path && path[k] == i;
+      v = penalized(v, c, bit, bias, (e.bits >> (16 + j)) & 1, pen);
+      if constexpr (OUT) {
+        if constexpr (BF16) out[i] = (uint16_t)f32_to_bf16_bits(v);
+        else out[i] = v;
+      } else if (v > SPEC_NEG_INF && before(v, i, bv, bi)) {
+        bv = v;
+        bi = i;
       }
+    }
+  };
+  if (wave == 0 && end > full) {
+    T e[8];
 #pragma unroll
-      for (int j = 0; j < kMaxStages; ++j) {
-        // the wave's 512 tokens hold it: one lane's chunk does
-        const uint32_t at = (uint32_t)path[j] - (uint32_t)__builtin_amdgcn_readfirstlane(i - lane * 8);
-        if (j < n_path && at < 512u) touched[u] |= lane == (int)(at >> 3) ? 1u << (at & 7) : 0u;
+    for (int j = 0; j < 8; ++j) e[j] = full + j < end ? row[full + j] : T(0);
+    s_raw[0][0] = load_words<words>(e);
+    uint32_t bits = ((1u << (end - full)) - 1) | 0xff0000;
+    if (pen.seen) bits |= (uint32_t)reinterpret_cast<const uint8_t*>(pen.seen)[full >> 3] << 8;
+    if (pen.allowed) bits &= 0xffff | (uint32_t)reinterpret_cast<const uint8_t*>(pen.allowed)[full >> 3] << 16;
+    s_list[0][0] = {(uint32_t)full >> 3, bits};
+    listed = 1;
+  }
+  for (int i0 = begin + tid * 8; i0 - tid * 8 < full; i0 += TRIP) {
+    uint32_t touched[CHUNKS], seen[CHUNKS], allow[CHUNKS];
+    words now[CHUNKS];
+#pragma unroll
+    for (int u = 0; u < CHUNKS; ++u) touched[u] = seen[u] = was_seen[u], allow[u] = ok[u], now[u] = x[u];
+    if (i0 - tid * 8 + TRIP < full) load(i0 + TRIP);
+    if (pen.counts && !pen.seen) {
+#pragma unroll
+      for (int u = 0; u < CHUNKS; ++u) {
+        const i32x8 c = load_words<i32x8>(pen.counts + min(i0 + u * STEP, full - 8));
+        touched[u] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) touched[u] |= c[j] ? 1u << j : 0u;
+      }
+    }
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane(i0 - lane * 8);
+#pragma unroll
+    for (int j = 0; j < kMaxStages; ++j) {
+      // the wave's 512 tokens of a chunk hold it: one lane's eight do
+      const uint32_t at = (uint32_t)path[j] - first;
+      if (j < n_path && at < (uint32_t)TRIP && at % STEP < 512u) {
+#pragma unroll
+        for (int u = 0; u < CHUNKS; ++u) touched[u] |= at / STEP == (uint32_t)u && lane == (int)(at % STEP >> 3) ? 1u << (at & 7) : 0u;
       }
     }
 #pragma unroll
-    for (int u = 0; u < kRowChunks; ++u) {
-      const int i = i0 + u * kRowThreads * 8;
-      if (i >= V) continue;
-      const int left = min(V - i, 8);
+    for (int u = 0; u < CHUNKS; ++u) {
+      const bool mine = touched[u] && i0 + u * STEP < full;
+      const uint64_t all = __ballot(mine);
+      if (mine) {
+        const int at = listed + __popcll(all & ((1ull << lane) - 1));
+        s_raw[wave][at] = now[u];
+        s_list[wave][at] = {(uint32_t)(i0 + u * STEP) >> 3, touched[u] | seen[u] << 8 | allow[u] << 16};
+      }
+      listed += __popcll(all);
+    }
+#pragma unroll
+    for (int u = 0; u < CHUNKS; ++u) {
+      const int i = i0 + u * STEP;
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if constexpr (BF16) v[j] = bf16_bits_to_f32((uint16_t)(x[u][j / 2] >> (j & 1) * 16));
-        else v[j] = __uint_as_float(x[u][j]);
+        if constexpr (BF16) v[j] = bf16_bits_to_f32((uint16_t)(now[u][j / 2] >> (j & 1) * 16));
+        else v[j] = __uint_as_float(now[u][j]);
       }
       if (pen.bias) {
-        floatx8 y = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (left == 8) {
-          y = load_words<floatx8>(pen.bias + i);
-        } else {
+        const floatx8 y = load_words<floatx8>(pen.bias + min(i, full - 8));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = j < left ? pen.bias[i + j] : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += OUT && ((touched[u] >> j) & 1) ? 0.0f : y[j];
+        for (int j = 0; j < 8; ++j) v[j] = OUT && ((touched[u] >> j) & 1) ? v[j] : v[j] + y[j];
       }
       if constexpr (OUT) {
-        const uint32_t gone = ~ok[u] & ~touched[u] & 0xff;
+        const uint32_t gone = ~allow[u] & ~touched[u] & 0xff;
         if (gone) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = (gone >> j) & 1 ? SPEC_NEG_INF : v[j];
         }
-        if (!pen.bias && !gone && p.out == p.logits) continue;
+        if (i >= full || (!pen.bias && !gone && p.out == p.logits)) continue;
         words w;
         if constexpr (BF16) {
 #pragma unroll
@@ -181,17 +244,9 @@ __global__ __launch_bounds__(kRowThreads, 4) void logits_kernel(LogitsJob p) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
         }
-        if (left == 8) {
-          __builtin_memcpy(out + i, &w, sizeof(w));
-        } else {
-          T e[8];
-          __builtin_memcpy(e, &w, sizeof(w));
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < left) out[i + j] = e[j];
-        }
+        __builtin_memcpy(out + i, &w, sizeof(w));
       } else {
-        const uint32_t gone = (touched[u] | ~ok[u] | 0xffu << left) & 0xff;
+        const uint32_t gone = i < full ? (touched[u] | ~allow[u]) & 0xff : 0xffu;
         if (gone) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = (gone >> j) & 1 ? SPEC_NEG_INF : v[j];
@@ -199,69 +254,38 @@ __global__ __launch_bounds__(kRowThreads, 4) void logits_kernel(LogitsJob p) {
         float m = v[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) m = fmaxf(m, v[j]);
-        if (m > bv) {   // (a thread meets its chunks in increasing order: the first maximum stays; NaN is never larger)
-          bv = m;
+        if (m >= bv && m > SPEC_NEG_INF) {   // (NaN is not)
+          int32_t c = i;
 #pragma unroll
           for (int j = 7; j >= 0; --j)
-            if (v[j] == m) bi = i + j;
+            if (v[j] == m) c = i + j;
+          if (m > bv || c < bi) bi = c;
+          bv = m;
         }
       }
     }
-    if (i0 - tid * 8 + kRowThreads * 8 * kRowChunks < V) load(i0 + kRowThreads * 8 * kRowChunks);
+    while (listed > 64) work_off();
   }
-
-  // ---- touched tokens (where logits and out are the same memory, these are still what they were) ----
-  auto touch = [&](int i, int c, bool bit) {
-#pragma unroll
-    for (int j = 0; j < kMaxStages; ++j) c += j < n_path && path[j] == i;
-    float v;
-    if constexpr (BF16) v = bf16_bits_to_f32(row[i]);
-    else v = row[i];
-    v = penalized(v, i, c, bit, pen);
-    if constexpr (OUT) {
-      if constexpr (BF16) out[i] = (uint16_t)f32_to_bf16_bits(v);
-      else out[i] = v;
-    } else if (v > SPEC_NEG_INF && before(v, i, bv, bi)) {
-      bv = v;
-      bi = i;
-    }
-  };
-  if (OUT) __syncthreads();
-  if (pen.seen || pen.counts)
-    for (int w = tid; w < n_words; w += kRowThreads) {
-      uint32_t bits = 0;
-      if (pen.seen) {
-        bits = pen.seen[w];
-        if (w * 32 + 32 > V) bits &= (1u << (V - w * 32)) - 1;
-      } else {
-        for (int j = 0; j < 32 && w * 32 + j < V; ++j) bits |= pen.counts[w * 32 + j] ? 1u << j : 0u;
-      }
-      while (bits) {
-        const int i = w * 32 + __builtin_ctz(bits);
-        bits &= bits - 1;
-        touch(i, pen.counts ? pen.counts[i] : 0, pen.seen != nullptr);
-      }
-    }
-  if (tid < n_path) {
-    const int i = s_path[tid];
-    bool first = (unsigned)i < (unsigned)V;
-    for (int j = 0; j < tid; ++j) first = first && s_path[j] != i;
-    if (first && !(pen.seen ? (pen.seen[i >> 5] >> (i & 31)) & 1 : pen.counts ? pen.counts[i] != 0 : 0)) touch(i, 0, false);
-  }
+  if (listed) work_off();
   if (OUT) return;
-  block_best<kRowThreads>(bv, bi, sv, si);
-  if (tid == 0) p.greedy[blockIdx.x] = bi == kIdxNone ? 0 : bi;
+  block_best<NT>(bv, bi, sv, si);
+  if (tid == 0) p.greedy[me] = bi == kIdxNone ? 0 : bi;
 }
 
 hipError_t launch_logits(const LogitsJob& job, bool bf16, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)job.batch * (job.M + 1))), block(kRowThreads);
-  const size_t smem = job.node_tok ? 2 * (size_t)job.M * sizeof(int32_t) : 0;
-  if (job.out) {
-    if (bf16) hipLaunchKernelGGL((logits_kernel<true, true>), grid, block, smem, st, job);
-    else hipLaunchKernelGGL((logits_kernel<false, true>), grid, block, smem, st, job);
+  const int64_t rows = (int64_t)job.batch * (job.M + 1);
+  const unsigned gx = (unsigned)(rows + 7) & ~7u;
+  if (job.out) {   // parts of a row where there are few: 64 rows of 32003 whole: 21 us, in eight: 8 us
+    const int parts = (int)min((int64_t)(job.V + 4095) / 4096, (1023 + rows) / rows), span = ((job.V + parts - 1) / parts + 31) & ~31;
+    const dim3 grid(gx, (unsigned)((job.V + span - 1) / span));
+    if (bf16) hipLaunchKernelGGL((logits_kernel<true, true, 512>), grid, dim3(512), 0, st, job, span);
+    else hipLaunchKernelGGL((logits_kernel<false, true, 512>), grid, dim3(512), 0, st, job, span);
+  } else if (rows <= kWideRows) {
+    if (bf16) hipLaunchKernelGGL((logits_kernel<true, false, 1024>), dim3(gx), dim3(1024), 0, st, job, 0);
+    else hipLaunchKernelGGL((logits_kernel<false, false, 1024>), dim3(gx), dim3(1024), 0, st, job, 0);
   } else {
-    if (bf16) hipLaunchKernelGGL((logits_kernel<true, false>), grid, block, smem, st, job);
-    else hipLaunchKernelGGL((logits_kernel<false, false>), grid, block, smem, st, job);
+    if (bf16) hipLaunchKernelGGL((logits_kernel<true, false, 512>), dim3(gx), dim3(512), 0, st, job, 0);
+    else hipLaunchKernelGGL((logits_kernel<false, false, 512>), dim3(gx), dim3(512), 0, st, job, 0);
   }
   return hipGetLastError();
 }
