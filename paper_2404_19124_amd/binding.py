@@ -161,8 +161,9 @@ def _native():
             raise RuntimeError("_call.so is missing or does not load: run `python -m paper_2404_19124_amd.build`; there is no "
                                "fallback path") from e
         at = [C.cast(f, C.c_void_p).value for f in (l.spec_verify, l.spec_verify_dynamic, l.spec_advance, l.spec_tree_metadata,
-                                                    l.spec_draft)]
-        _call.bind(*at, lambda stream: _stream_ptr(stream))
+                                                    l.spec_draft, l.spec_tree_attention, l.spec_cache_extend, l.spec_cache_store,
+                                                    l.spec_penalize, l.spec_verify_tree)]
+        _call.bind(*at[:5], lambda stream: _stream_ptr(stream), *at[5:])
         _fast = _call
     return _fast
 
@@ -604,6 +605,9 @@ def spec_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tenso
     kv_heads, head_dim]: any strides but along head_dim, rows on 16 bytes, the same strides in k_* and v_*.  node_parent [batch, M]
     (None: M = 0), n_nodes [batch] (None: M each).  workspace: contiguous uint8, spec_tree_attention_workspace() bytes, not
     shared by calls that may overlap in time.  scale: head_dim ** -0.5 by default."""
+    if _CHECK_DEVICE and _done((_fast or _native()).tree_attention(
+            q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, node_parent, n_nodes, out, workspace, scale, stream)):
+        return
     code = _float_code(q, "q", (4,))
     b, R, H, D = q.shape
     if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
@@ -646,6 +650,10 @@ def spec_cache_extend(ctx_len: torch.Tensor, add: torch.Tensor, new_len: torch.T
     ctx_len, add, new_len, added [batch]; block_table [batch, max_blocks]; ring [n_blocks]; ring_state, ring_state_new [2];
     row_start [batch + 1]; slot, pos, src_row [cap]; path_row [batch, path_width] with src_row: all int32.  new_len may be
     ctx_len and ring_state_new may be ring_state; no other two may share memory."""
+    if _CHECK_DEVICE and _done((_fast or _native()).cache_extend(
+            ctx_len, add, new_len, added, block_table, ring, ring_state, ring_state_new, block_size, row_start, slot, pos, path_row, seq_rows,
+            src_row, stream)):
+        return
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or not isinstance(ring, torch.Tensor) or ring.dim() != 1:
         raise ValueError("block_table must be a [batch, max_blocks] tensor and ring a [n_blocks] tensor")
     if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
@@ -683,6 +691,9 @@ def spec_cache_store(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tenso
 
     One layer: k_new, v_new [rows, kv_heads, head_dim], k_cache, v_cache [n_blocks, block_size, kv_heads, head_dim].  Several at
     once: a first dimension of layers in all four.  Strides as for spec_tree_attention; slot, src_row [count] int32."""
+    if _CHECK_DEVICE and _done((_fast or _native()).cache_store(
+            k_new, v_new, slot, k_cache, v_cache, src_row, stream)):
+        return
     code = _float_code(k_cache, "k_cache", (4, 5))
     if not isinstance(k_new, torch.Tensor) or not isinstance(v_new, torch.Tensor) or not isinstance(v_cache, torch.Tensor):
         raise ValueError("k_new, v_new and v_cache must be tensors")
@@ -698,6 +709,7 @@ def spec_cache_store(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tenso
     if ck != cv or sk != sv:
         raise ValueError("k_cache and v_cache, and k_new and v_new, must have the same strides")
     _written(k_cache, "k_cache")
+    _written(v_cache, "v_cache")
     if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
         raise ValueError("slot must be a [count] tensor")
     count = int(slot.shape[0])
@@ -737,6 +749,8 @@ def spec_penalize(logits: torch.Tensor, out: torch.Tensor, penalties: Dict[str, 
     penalties: any of counts [batch, vocab] int32, seen [batch, W] int32, repetition / presence / frequency [batch] float32,
     bias [n_bias, vocab] float32 with bias_row [batch] int32, allowed [n_allowed, W] int32 with mask_row [batch, R] int32, where
     W = ceil(vocab / 32) words of 32 bits, the lowest first.  node_tok, node_parent [batch, R - 1]: rows count the tokens on their path."""
+    if _CHECK_DEVICE and _done((_fast or _native()).penalize(logits, out, penalties, node_tok, node_parent, n_nodes, stream)):
+        return
     code = _float_code(logits, "logits", (3,))
     b, R, V = logits.shape
     if R < 1:
@@ -765,6 +779,10 @@ def spec_verify_tree(logits: torch.Tensor, cand_tokens: torch.Tensor, cand_node:
     cand_tokens, cand_node [batch, B, n] (n = 0 and B = 1: plain decoding); greedy [batch, R]; accept_len, best_cand, n_out
     [batch]; out_tokens, path_row [batch, n + 1]; accept_all [batch, B].  update: the emitted tokens are added to
     penalties' counts and seen."""
+    if _CHECK_DEVICE and _done((_fast or _native()).verify_tree(
+            logits, cand_tokens, cand_node, n_nodes, greedy, accept_len, best_cand, out_tokens, n_out, path_row, accept_all, n_cand,
+            penalties, node_tok, node_parent, update, stream)):
+        return
     code = _float_code(logits, "logits", (3,))
     b, R, V = logits.shape
     if R < 1:
