@@ -54,15 +54,16 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 typedef const __attribute__((address_space(4))) int32_t* scalar_i32;
 
 // The work is cut into equal shares by COST: a unit costs its tiles and kUnitCost more for its queries and results (a sequence
-// with nothing cached, 24 units of one tile in one share: that workgroup took a third longer than all others).
-constexpr int kUnitCost = 1;
+// with nothing cached, 24 units of one tile in one share: that workgroup took a third longer than all others).  32 sequences of
+// 8 key/value heads with 368 query rows: 0: 298 us, 1: 240 us, 2: 221 us, 3: 233 us; float32 tiles take longer, and a cost of 1 is best.
+constexpr int unit_cost(bool bf16) { return bf16 ? 2 : 1; }
 
 struct SeqTiles {
   int ctx, nodes, tiles, blocks;   // cached tokens, last row, tiles per unit, units per key/value head
   uint64_t total;                  // cost of all units
 };
 template <bool UNIFORM = false>
-__device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int BM) {
+__device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int BM, int unit_cost) {
   SeqTiles s;
   int ctx, nodes;
   if (UNIFORM) {
@@ -76,7 +77,7 @@ __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int 
   s.nodes = min(max(nodes, -1), p.M);
   s.tiles = (s.ctx + s.nodes + KT) / KT;
   s.blocks = (int)(((int64_t)(s.nodes + 1) * (p.q_heads / p.kv_heads) + BM - 1) / BM);
-  s.total = (uint64_t)(s.tiles + kUnitCost) * (uint64_t)s.blocks * (uint64_t)p.kv_heads;
+  s.total = (uint64_t)(s.tiles + unit_cost) * (uint64_t)s.blocks * (uint64_t)p.kv_heads;
   return s;
 }
 
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   typedef AttentionShape<BF16, DP, MQ, WK> S;
   typedef AttentionTile<BF16, DP, MQ, WK> Tile;
   typedef TileCopy<BF16, DP, MQ, WK> Copy;
-  constexpr int ESZ = S::ESZ, BM = S::BM;
+  constexpr int ESZ = S::ESZ, BM = S::BM, kUnitCost = unit_cost(BF16);
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   __shared__ uint32_t s_valid[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   // and values) and no unit cost, 244 us so ----
   uint64_t all = 0;
   for (int q0 = 0; q0 < p.batch; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM).total : 0;
+    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, kUnitCost).total : 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
     all += t;
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   int q = 0;
   uint64_t start = 0;   // of sequence q
   for (int q0 = 0;; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM).total : 0, sum = t;
+    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, kUnitCost).total : 0, sum = t;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const uint64_t y = __shfl_up((unsigned long long)sum, d);
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 
   // ---- segments ----
   auto of_sequence = [&](Segment& s, int seq) {
-    const SeqTiles t = seq_tiles<true>(p, seq, BM);
+    const SeqTiles t = seq_tiles<true>(p, seq, BM, kUnitCost);
     s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
     s.heads = uniform(min(max(share / (t.tiles + kUnitCost), 1), p.kv_heads));
     return t.total;
