@@ -25,6 +25,7 @@ typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int KT = 64;   // keys of a tile
+constexpr float kSlack = 8;
 
 // larger / sum of a value and those of the lanes 16 and 32 away: the same query row's other keys
 __device__ __forceinline__ float groups_max(float x) {
@@ -125,27 +126,36 @@ struct AttentionTile {
     constexpr int ROWB = S::ROWB, KW = S::KW, NB = S::NB, SWZ = S::SWZ;
     const int tid = opaque_tid(), lane = tid & 63, l16 = lane & 15, grp = lane >> 4, wk = (tid >> 6) % WK;
     // ---- scores, transposed: keys 4 grp + i of a block in the lane's registers, query row l16 ----
+    // The reads of the next block of keys are sent before the products of one, and nothing is moved across the line between
+    // them: the compiler by itself waits for nearly every read right behind it, in registers that it uses for all of them.
     f32x4 s[MQ][NB];
+    u32x4 kf[2][QS];
+    auto read_keys = [&](int nb) {
+      const int key = wk * KW + nb * 16 + l16;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) kf[nb & 1][st] = *reinterpret_cast<const lds_u32x4*>(kb + key * ROWB + (((st * 4 + grp) ^ (key & SWZ)) * 16));
+    };
+    read_keys(0);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int key = wk * KW + nb * 16 + l16;
-      const lds_u8* row = kb + key * ROWB;
+      if (nb + 1 < NB) read_keys(nb + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) s[mq][nb] = (f32x4){0, 0, 0, 0};
 #pragma unroll
       for (int st = 0; st < QS; ++st) {
-        const u32x4 raw = *reinterpret_cast<const lds_u32x4*>(row + (((st * 4 + grp) ^ (key & SWZ)) * 16));
-        const qword kf = __builtin_bit_cast(qword, raw);
+        const qword f = __builtin_bit_cast(qword, kf[nb & 1][st]);
 #pragma unroll
         for (int mq = 0; mq < MQ; ++mq) {
           if constexpr (BF16) {
-            s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mq][st], s[mq][nb], 0, 0, 0);
+            s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[mq][st], s[mq][nb], 0, 0, 0);
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[mq][st][e], s[mq][nb], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) s[mq][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], qf[mq][st][e], s[mq][nb], 0, 0, 0);
           }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
 
     // ---- which of the tile's keys a row sees ----
@@ -175,6 +185,22 @@ struct AttentionTile {
       }
     }
 
+    // ---- values.  The weights are in the place that the product wants them in if the values' keys are taken in the same
+    // order: 4 grp + i of a block, then of the next.  Two blocks of the head's elements are read ahead, the first ones before the
+    // exponentials ----
+    constexpr int ND = DP / 16, AHEAD = 2;
+    i16x4 vf[AHEAD + 1][NB];
+    auto read_values = [&](int d) {
+      if constexpr (BF16) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int key = wk * KW + nb * 16 + grp * 4 + (l16 >> 2), word = (d * 2 + ((l16 & 3) >> 1)) ^ (key & SWZ);
+          // (16 lanes read four keys' 16 elements, and each gets one element of the four keys)
+          vf[d % (AHEAD + 1)][nb] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + key * ROWB + word * 16 + (l16 & 1) * 8));
+        }
+      }
+    };
+
     // ---- softmax: weights relative to the running maximum ----
 #pragma unroll
     for (int mq = 0; mq < MQ; ++mq) {
@@ -184,7 +210,9 @@ struct AttentionTile {
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mq][nb][i]);
       top = groups_max(top) * sc;
-      if (__any(top > m_run[mq])) {
+      // (weights may grow to 2^8 before the maximum they are relative to is moved: what is summed is float32, and rounding a weight
+      // to bfloat16 is relative.  Moving it with every larger product: 128 of a tile's 330 vector instructions)
+      if (__any(top > m_run[mq] + kSlack)) {
         const float m_new = fmaxf(m_run[mq], top), keep = __builtin_amdgcn_exp2f(m_run[mq] - m_new);
         m_run[mq] = m_new;
         l_run[mq] *= keep;
@@ -193,6 +221,14 @@ struct AttentionTile {
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[mq][d][i] *= keep;
       }
+    }
+    if constexpr (BF16) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) read_values(d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int mq = 0; mq < MQ; ++mq) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -203,14 +239,7 @@ struct AttentionTile {
         }
     }
 
-    // ---- values.  The weights are in the place that the product wants them in if the values' keys are taken in the same
-    // order: 4 grp + i of a block, then of the next ----
     if constexpr (BF16) {
-      auto values = [&](int nb, int d) -> i16x4 {
-        const int key = wk * KW + nb * 16 + grp * 4 + (l16 >> 2), word = (d * 2 + ((l16 & 3) >> 1)) ^ (key & SWZ);
-        // (16 lanes read four keys' 16 elements, and each gets one element of the four keys)
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + key * ROWB + word * 16 + (l16 & 1) * 8));
-      };
       if constexpr (NB == 1) {
         i16x4 w[MQ];
 #pragma unroll
@@ -220,9 +249,11 @@ struct AttentionTile {
         }
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
-          const i16x4 v = values(0, d);
+          if (d + AHEAD < ND) read_values(d + AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, w[mq], o[mq][d], 0, 0, 0);
+          for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[d % (AHEAD + 1)][0], w[mq], o[mq][d], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       } else {
         bf16x8 w[MQ][NB / 2];
@@ -235,28 +266,38 @@ struct AttentionTile {
             w[mq][j] = __builtin_bit_cast(bf16x8, raw);
           }
 #pragma unroll
-        for (int d = 0; d < DP / 16; ++d)
+        for (int d = 0; d < ND; ++d) {
+          if (d + AHEAD < ND) read_values(d + AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < NB / 2; ++j) {
-            const i16x4 a = values(2 * j, d), b = values(2 * j + 1, d);
+            const i16x4 a = vf[d % (AHEAD + 1)][2 * j], b = vf[d % (AHEAD + 1)][2 * j + 1];
             const bf16x8 v = __builtin_bit_cast(bf16x8, (i16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
 #pragma unroll
             for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[mq][j], o[mq][d], 0, 0, 0);
           }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     } else {
+      float vr[2][ND];
+      auto read_key = [&](int x) {
+        const int key = wk * KW + (x >> 2) * 16 + grp * 4 + (x & 3);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+        for (int d = 0; d < ND; ++d)
+          vr[x & 1][d] = *reinterpret_cast<const lds_f32*>(vb + key * ROWB + ((d * 4 + (l16 >> 2)) ^ (key & SWZ)) * 16 + (l16 & 3) * 4);
+      };
+      read_key(0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = wk * KW + nb * 16 + grp * 4 + i;
+      for (int x = 0; x < NB * 4; ++x) {
+        if (x + 1 < NB * 4) read_key(x + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int d = 0; d < DP / 16; ++d) {
-            const float v = *reinterpret_cast<const lds_f32*>(vb + key * ROWB + ((d * 4 + (l16 >> 2)) ^ (key & SWZ)) * 16 + (l16 & 3) * 4);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[mq][nb][i], o[mq][d], 0, 0, 0);
-          }
-        }
+          for (int mq = 0; mq < MQ; ++mq) o[mq][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[x & 1][d], s[mq][x >> 2][x & 3], o[mq][d], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
 };
@@ -307,8 +348,8 @@ struct TileCopy {
     int64_t at;
     int base;
   };
-  // the tile that is copied next, where it has no single place: this lane's address (bit 0: not in the cache) and which of
-  // the wave's rows are cached tokens
+  // the tile that is copied next, where it has no single place: this lane's offset from the head's keys in the cache, or (bit 0)
+  // from those of the tree's rows, and which of the wave's rows are cached tokens
   struct Rows {
     uint64_t at;
     uint32_t valid;
@@ -341,16 +382,16 @@ struct TileCopy {
   __device__ __forceinline__ Rows rows_of(const Segment& s, int t) const {
     const int tid = opaque_tid(), key = (s.tile0 + t) * KT + (tid >> 6) * RW + (tid & 63) % RW;
     // what is not a key is read from row 0, which every row sees: with a weight of zero it adds nothing
-    uint64_t a = reinterpret_cast<uint64_t>(s.k_rows) | 1;
+    uint64_t a = 1;
     bool ok = false;
     if (key < s.ctx) {
       const int b = key / p.block_size, x = p.block_table[(int64_t)s.q * p.max_blocks + b];
       if (x >= 0 && x < p.n_blocks) {
-        a = reinterpret_cast<uint64_t>(s.k_cache + x * p.block + (key - b * p.block_size) * p.slot);
+        a = (uint64_t)(x * p.block + (key - b * p.block_size) * p.slot);
         ok = true;
       }
     } else if (key < s.keys) {
-      a = reinterpret_cast<uint64_t>(s.k_rows + (int64_t)(key - s.ctx) * p.new_row) | 1;
+      a = (uint64_t)((key - s.ctx) * p.new_row) | 1;
     }
     return {a, (uint32_t)__ballot(ok) & ((1u << RW) - 1)};
   }
@@ -361,8 +402,10 @@ struct TileCopy {
     if (place_of(f, t) < 0) r = rows_of(s, t);
   }
 
-  __device__ __forceinline__ static void copy16(const uint8_t* from, lds_u8* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  // (as buffer instructions: behind copies into LDS that go through flat addresses, the compiler waits for all LDS reads at once)
+  __device__ __forceinline__ static void copy16(const uint8_t* from, uint32_t offset, lds_u8* to) {
+    const auto place = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, -1, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(place, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
   }
   // a lane's 16 bytes land at its place in the instruction's 1 KiB: the words of a row are permuted where they are read
   __device__ __forceinline__ void copy(const Segment& s, int t, const Places& f, const Rows& r, lds_u8* to, uint32_t* valid) const {
@@ -374,19 +417,36 @@ struct TileCopy {
       const uint8_t *k = s.k_cache + place, *v = k + to_v_cache;
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
-        copy16(k + offset[j], at + j * RPI * S::ROWB);
-        copy16(v + offset[j], at + (KT + j * RPI) * S::ROWB);
+        copy16(k, offset[j], at + j * RPI * S::ROWB);
+        copy16(v, offset[j], at + (KT + j * RPI) * S::ROWB);
       }
       return;
     }
     if (lane == 0) valid[wave] = r.valid;
+    if (p.offsets_fit) {
 #pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int row = j * RPI + lane / S::CH, word = (lane % S::CH) ^ ((wave * RW + row) & S::SWZ);
-      const uint64_t x = __shfl((unsigned long long)r.at, row);
-      const uint8_t* k = reinterpret_cast<const uint8_t*>(x & ~1ull) + min(word, last_word) * 16;
-      copy16(k, at + j * RPI * S::ROWB);
-      copy16(k + (x & 1 ? to_v_rows : to_v_cache), at + (KT + j * RPI) * S::ROWB);
+      for (int j = 0; j < NL; ++j) {
+        const int row = j * RPI + lane / S::CH, word = min((lane % S::CH) ^ ((wave * RW + row) & S::SWZ), last_word);
+        const uint32_t x = (uint32_t)__shfl((int)r.at, row), from = (x & ~1u) + word * 16;
+        lds_u8 *k = at + j * RPI * S::ROWB, *v = at + (KT + j * RPI) * S::ROWB;
+        if (x & 1) {
+          copy16(s.k_rows, from, k);
+          copy16(s.k_rows + to_v_rows, from, v);
+        } else {
+          copy16(s.k_cache, from, k);
+          copy16(s.k_cache + to_v_cache, from, v);
+        }
+      }
+      return;
+    }
+    for (int row = 0; row < RW; ++row) {   // (a cache of more than 4 GiB) row by row, by the lanes whose words are theirs
+      const uint64_t x = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(r.at >> 32), row) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)r.at, row);
+      const uint8_t *k = (x & 1 ? s.k_rows : s.k_cache) + (x & ~1ull), *v = k + (x & 1 ? to_v_rows : to_v_cache);
+      const int word = (lane % S::CH) ^ ((wave * RW + row) & S::SWZ), j = row / RPI;
+      if (lane / S::CH == row % RPI) {
+        copy16(k, min(word, last_word) * 16, at + j * RPI * S::ROWB);
+        copy16(v, min(word, last_word) * 16, at + (KT + j * RPI) * S::ROWB);
+      }
     }
   }
 };

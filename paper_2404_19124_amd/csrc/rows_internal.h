@@ -20,6 +20,7 @@ struct AttentionJob {
   const int32_t *block_table, *ctx_len, *node_parent, *n_nodes;
   int batch, M, q_heads, kv_heads, head_dim;
   int max_blocks, n_blocks, block_size;
+  int offsets_fit; // every key lies within 4 GiB of its head's first one, in the cache and among the rows
   int one_place;   // 16 tokens from a multiple of 16 on lie in one block, at offsets of 31 bits
   float scale;
   void* workspace;

@@ -85,6 +85,10 @@ extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_ro
   j.batch = batch, j.M = M, j.q_heads = q_heads, j.kv_heads = kv_heads, j.head_dim = head_dim;
   j.max_blocks = max_blocks, j.n_blocks = cache->n_blocks, j.block_size = cache->block_size;
   j.one_place = cache->block_size % 16 == 0 && j.slot >= 0 && j.slot < (1 << 26);
+  // (strides of 2^31 and more do not multiply beyond 63 bits: a tensor's bytes are addressable)
+  const int64_t most = (1ll << 32) - 64 - head_dim * esz;
+  j.offsets_fit = j.block >= 0 && j.slot >= 0 && j.new_row >= 0 && j.new_row * M <= most &&
+                  j.block * (cache->n_blocks - 1) + j.slot * (cache->block_size - 1) <= most;
   j.scale = scale, j.workspace = workspace;
   HIP_TRY(launch_attention(j, dtype == SPEC_BF16, static_cast<hipStream_t>(hip_stream)));
   return SPEC_OK;
