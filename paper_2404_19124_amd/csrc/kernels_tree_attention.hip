@@ -396,25 +396,32 @@ struct TileCopy {
     return {a, (uint32_t)__ballot(ok) & ((1u << RW) - 1)};
   }
 
-  // what copying tile t will need; called for the tiles of a segment one after the other
-  __device__ __forceinline__ void prepare(const Segment& s, int t, Places& f, Rows& r) const {
+  // what copying a tile needs
+  struct Source {
+    uint64_t k_cache, k_rows;   // addresses of the head's; 0: nothing to copy
+    int64_t place;              // -1: row by row
+    Rows r;
+  };
+  // of tile t of a segment; called for its tiles one after the other
+  __device__ __forceinline__ Source source(const Segment& s, int t, Places& f) const {
     if (t - f.base == 64) f = places(s, t);
-    if (place_of(f, t) < 0) r = rows_of(s, t);
+    Source x = {reinterpret_cast<uint64_t>(s.k_cache), reinterpret_cast<uint64_t>(s.k_rows), place_of(f, t), {0, 0}};
+    if (x.place < 0) x.r = rows_of(s, t);
+    return x;
   }
 
   // (as buffer instructions: behind copies into LDS that go through flat addresses, the compiler waits for all LDS reads at once)
-  __device__ __forceinline__ static void copy16(const uint8_t* from, uint32_t offset, lds_u8* to) {
-    const auto place = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, -1, 0x00020000);
+  __device__ __forceinline__ static void copy16(uint64_t from, uint32_t offset, lds_u8* to) {
+    const auto place = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(uniform(from)), 0, -1, 0x00020000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(place, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
   }
   // a lane's 16 bytes land at its place in the instruction's 1 KiB: the words of a row are permuted where they are read
-  __device__ __forceinline__ void copy(const Segment& s, int t, const Places& f, const Rows& r, lds_u8* to, uint32_t* valid) const {
+  __device__ __forceinline__ void copy(const Source& s, lds_u8* to, uint32_t* valid) const {
     const int tid = opaque_tid(), lane = tid & 63, wave = uniform(tid >> 6);
     lds_u8* at = to + wave * RW * S::ROWB;
-    const int64_t place = place_of(f, t);
-    if (place >= 0) {
+    if (s.place >= 0) {
       if (lane == 0) valid[wave] = (1u << RW) - 1;
-      const uint8_t *k = s.k_cache + place, *v = k + to_v_cache;
+      const uint64_t k = s.k_cache + s.place, v = k + to_v_cache;
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
         copy16(k, offset[j], at + j * RPI * S::ROWB);
@@ -422,26 +429,28 @@ struct TileCopy {
       }
       return;
     }
-    if (lane == 0) valid[wave] = r.valid;
+    if (lane == 0) valid[wave] = s.r.valid;
+    const uint64_t k_cache = s.k_cache, k_rows = s.k_rows;
     if (p.offsets_fit) {
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
         const int row = j * RPI + lane / S::CH, word = min((lane % S::CH) ^ ((wave * RW + row) & S::SWZ), last_word);
-        const uint32_t x = (uint32_t)__shfl((int)r.at, row), from = (x & ~1u) + word * 16;
+        const uint32_t x = (uint32_t)__shfl((int)s.r.at, row), from = (x & ~1u) + word * 16;
         lds_u8 *k = at + j * RPI * S::ROWB, *v = at + (KT + j * RPI) * S::ROWB;
         if (x & 1) {
-          copy16(s.k_rows, from, k);
-          copy16(s.k_rows + to_v_rows, from, v);
+          copy16(k_rows, from, k);
+          copy16(k_rows + to_v_rows, from, v);
         } else {
-          copy16(s.k_cache, from, k);
-          copy16(s.k_cache + to_v_cache, from, v);
+          copy16(k_cache, from, k);
+          copy16(k_cache + to_v_cache, from, v);
         }
       }
       return;
     }
+#pragma unroll 1
     for (int row = 0; row < RW; ++row) {   // (a cache of more than 4 GiB) row by row, by the lanes whose words are theirs
-      const uint64_t x = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(r.at >> 32), row) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)r.at, row);
-      const uint8_t *k = (x & 1 ? s.k_rows : s.k_cache) + (x & ~1ull), *v = k + (x & 1 ? to_v_rows : to_v_cache);
+      const uint64_t x = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(s.r.at >> 32), row) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)s.r.at, row);
+      const uint64_t k = (x & ~1ull) + (x & 1 ? k_rows : k_cache), v = k + (x & 1 ? to_v_rows : to_v_cache);
       const int word = (lane % S::CH) ^ ((wave * RW + row) & S::SWZ), j = row / RPI;
       if (lane / S::CH == row % RPI) {
         copy16(k, min(word, last_word) * 16, at + j * RPI * S::ROWB);
@@ -572,9 +581,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
                static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new)};
   copy.init();
   typename Copy::Places f = copy.places(now, 0), f_next = {-1, 0};
-  typename Copy::Rows r = {0, 0}, r_next = {0, 0};
-  copy.prepare(now, 0, f, r);
-  copy.copy(now, 0, f, r, (lds_u8*)smem, s_valid[0]);
+  copy.copy(copy.source(now, 0, f), (lds_u8*)smem, s_valid[0]);
   int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
   while (more) {
     Segment next = now;
@@ -610,21 +617,23 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d) x.o[mq][d] = (f32x4){0, 0, 0, 0};
     }
-    if (now.n_tiles > 1) copy.prepare(now, 1, f, r);
+    typename Copy::Source first = {0, 0, 0, {0, 0}}, up;   // of the next segment; what is copied next
     if (more) {
       f_next = copy.places(next, 0);
-      copy.prepare(next, 0, f_next, r_next);
+      first = copy.source(next, 0, f_next);
     }
+    if (now.n_tiles > 1) up = copy.source(now, 1, f);
+    else up = first;
 
     // ---- tiles.  The next one is copied into the other buffer while one is worked on; the two buffers are distinct objects to
     // the compiler (restrict), so that a read of one does not wait for the copies into the other ----
     auto tile = [&](lds_u8* cur, lds_u8* other, int t) {
       attention_turn<BF16, DP, MQ, WK>(
           x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, [&](lds_u8* to) {
-            if (t + 1 < now.n_tiles) copy.copy(now, t + 1, f, r, to, s_valid[(turn + 1) & 1]);
-            else if (more) copy.copy(next, 0, f_next, r_next, to, s_valid[(turn + 1) & 1]);
+            if (up.k_cache) copy.copy(up, to, s_valid[(turn + 1) & 1]);
           });
-      if (t + 2 < now.n_tiles) copy.prepare(now, t + 2, f, r);
+      if (t + 2 < now.n_tiles) up = copy.source(now, t + 2, f);
+      else up = first;
       ++turn;
     };
     for (int t = 0; t < now.n_tiles;) {
@@ -703,7 +712,6 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     unit_end += (uint64_t)(next.tiles + kUnitCost);
     now = next;
     f = f_next;
-    r = r_next;
     ++n_units;
   }
   if (tid == 0) ws.owner[me] = mine;
