@@ -170,3 +170,18 @@ def test_nothing_to_store():
     B.spec_cache_store(torch.zeros((0, 1, 8), device="cuda"), torch.zeros((0, 1, 8), device="cuda"),
                        torch.zeros((2,), dtype=torch.int32, device="cuda"), kc, kc.clone(), torch.zeros((2,), dtype=torch.int32, device="cuda"))
     assert (kc == 0).all()
+
+
+@pytest.mark.parametrize("b,cap", [(1, 4096), (1, 4097), (1024, 4096), (1024, 4097), (1025, 4096), (1023, 500)])
+def test_where_one_kernel_becomes_two(b, cap):
+    """Up to 1024 sequences and 4096 entries of the slot map are one kernel, more are two."""
+    rng = np.random.default_rng(b + cap)
+    s = Server(rng, b, 16, [0] * b, 1500, 700)
+    s.step([1 + q % 7 for q in range(b)], cap=cap)
+    add = [int(x) for x in rng.integers(-5, 20, b)]
+    add[b // 2] = 6000                      # more than the blocks or the slot map, or just within
+    s.step(add, cap=cap)
+    add = [-3] * b
+    add[b // 2] = 9000 if b == 1 else -10 ** 6
+    s.step(add, cap=cap, in_place=True)
+    s.step([1] * b, cap=cap, path=[[4, 2]] * b, seq_rows=5)
