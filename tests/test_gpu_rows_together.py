@@ -167,6 +167,8 @@ def test_steps_emit_what_decoding_token_by_token_does(captured, none_right):
             for c in range(C):      # candidates that are right for 0 to N tokens
                 right = int(rng.integers(0, N + 1)) if step % 3 else c % 2
                 cand[slot, c, :right] = true[:right]
+            if none_right:
+                cand[slot, :, 0] = (true[0] + 1) % V
         for slot, tokens in enumerate(s.step(cand.tolist())):
             if slot not in of:
                 assert tokens == []
