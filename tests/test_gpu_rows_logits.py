@@ -281,3 +281,80 @@ def test_a_large_vocabulary(dtype):
                 v = v + pen["bias"][int(pen["bias_row"][q])]
             rows.append(int(torch.nonzero(v == v.max())[0]))
         assert got["greedy"][q, :len(rows)].tolist() == rows
+
+
+# ---- calls of more rows than fit the card at once, whole rows per workgroup, several turns per row --------------------------
+
+def every_row_on_the_device(r):
+    """Processed logits in float32 on the device, one operation after the other, without paths."""
+    V, pen = r.V, r.dev_pen()
+    t = torch.arange(V, device="cuda")
+    bit = lambda words: ((words[:, t // 32] >> (t % 32)) & 1) > 0
+    seen = bit(pen["seen"])
+    c = torch.where(seen, pen["counts"], 0)
+    v = r.logits.float()
+    per = lambda k: pen[k][:, None, None]
+    v = torch.where((seen | (c > 0))[:, None], torch.where(v > 0, v / per("repetition"), v * per("repetition")), v)
+    v = v - (pen["frequency"][:, None] * c)[:, None]
+    v = torch.where((c > 0)[:, None], v - per("presence"), v)
+    row = pen["bias_row"].long()
+    v = torch.where(((row >= 0) & (row < 3))[:, None, None], v + pen["bias"][row.clamp(0, 2)][:, None], v)
+    row = pen["mask_row"].long()
+    ok = bit(pen["allowed"])[row.clamp(0, 4)] | ((row < 0) | (row >= 5))[..., None]
+    return torch.where(ok, v, float("-inf"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8192, 9005])
+def test_many_rows(dtype, V):
+    r = Rows(40, 29, V, dtype, seed=V, n_nodes=[29 - q % 3 for q in range(40)])
+    want = every_row_on_the_device(r)
+    out, work = torch.full_like(r.logits, 7.0), r.logits.clone()
+    args = (r.dev_pen(), None, None, dev(r.n_nodes))
+    B.spec_penalize(r.logits, out, *args)
+    B.spec_penalize(work, work, *args)
+    B_, n = 2, 3
+    cand, node = torch.zeros((40, B_, n), dtype=torch.int32, device="cuda"), torch.zeros((40, B_, n), dtype=torch.int32, device="cuda")
+    got = [torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((40, 30), (40,), (40,), (40, n + 1), (40,), (40, n + 1))]
+    B.spec_verify_tree(r.logits, cand, node, dev(r.n_nodes), *got, penalties=args[0])
+    for q, m in enumerate(r.n_nodes + 1):
+        assert torch.equal(out[q, :m], want[q, :m].to(r.dtype)) and (out[q, m:] == 7).all()
+        assert torch.equal(work[q, :m], out[q, :m]) and torch.equal(work[q, m:], r.logits[q, m:])
+        best = want[q, :m].max(-1, keepdim=True).values
+        first = (want[q, :m] == best).int().argmax(-1)
+        assert torch.equal(got[0][q, :m], first.int()) and (got[0][q, m:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_captured_replayed_and_on_another_stream(dtype):
+    """The captured call reads what its arguments hold at the replay; a call on another stream while it runs does not disturb it."""
+    r, cand, node = agreeing(3, 8, 3, 4099, dtype, seed=31)
+    others = [agreeing(3, 8, 3, 4099, dtype, seed=s) for s in (32, 33)]
+    a = dict(logits=r.logits.clone(), cand_tokens=dev(cand), cand_node=dev(node), n_nodes=dev(r.n_nodes), node_tok=dev(r.tok),
+             node_parent=dev(r.parent), penalties=r.dev_pen())
+    new = lambda: {k: torch.full(s, -9, dtype=torch.int32, device="cuda") for k, s in (
+        ("greedy", (3, r.R)), ("accept_len", (3,)), ("best_cand", (3,)), ("out_tokens", (3, 4)), ("n_out", (3,)), ("path_row", (3, 4)))}
+    got, soft = new(), torch.zeros_like(r.logits)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        B.spec_penalize(a["logits"], soft, a["penalties"], a["node_tok"], a["node_parent"], a["n_nodes"])
+        B.spec_verify_tree(**a, **got)
+    for x, xc, xn in [(r, cand, node)] + others + [(r, cand, node)]:
+        a["logits"].copy_(x.logits)
+        for name, t in (("cand_tokens", xc), ("cand_node", xn), ("n_nodes", x.n_nodes), ("node_tok", x.tok), ("node_parent", x.parent)):
+            a[name].copy_(dev(t))
+        for k, t in x.dev_pen().items():
+            a["penalties"][k].copy_(t)
+        torch.cuda.synchronize()
+        graph.replay()
+        mine, eager = new(), torch.full_like(soft, 7.0)
+        with torch.cuda.stream(side):
+            B.spec_penalize(a["logits"], eager, a["penalties"], a["node_tok"], a["node_parent"], a["n_nodes"])
+        B.spec_verify_tree(**a, **mine, stream=side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], mine[k]) for k in got)
+        want = RO.verify_tree(x.oracle(np.float32)[0], xc, xn, x.n_nodes, None)
+        assert all(np.array_equal(got[k].cpu().numpy(), want[k]) for k in got)
+        for q, m in enumerate(x.n_nodes + 1):
+            assert torch.equal(soft[q, :m], eager[q, :m])
