@@ -82,6 +82,10 @@ __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int 
   return s;
 }
 
+// Shares of up to this cost go to one workgroup per CU, more of them to two: 4 sequences of 32 heads, 10 tiles a share: 28.9 us with
+// one, 30.8 us with two; 24 sequences of one key/value head, 31 tiles a share: 86 us and 75 us.
+constexpr uint64_t kFewCost = 20;
+
 // What a workgroup that ends inside a unit leaves: see the join below.
 struct Owner {
   int q, g, block, last;   // the unit that starts in this workgroup and ends in workgroup `last`; q < 0: none
@@ -89,7 +93,8 @@ struct Owner {
 };
 
 struct AttentionSpace {
-  Owner* owner;     // [groups]
+  int* live;        // workgroups that have a share
+  Owner* owner;     // [groups], of those
   float* part;      // [groups][2][BM][DP + 4]: o, m, l of the segment that goes on from an earlier workgroup, of the one that
                     // goes on to a later one
   int groups;       // workgroups of the launch
@@ -484,13 +489,12 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
     all += t;
   }
-  const int me = (int)(blockIdx.x % 8) * (ws.groups / 8) + (int)(blockIdx.x / 8);
   all = uniform(all);
-  const uint64_t groups = min((uint64_t)ws.groups, (all + ws.least - 1) / ws.least);
-  if (me >= (int)groups) {
-    if (tid == 0) ws.owner[me].q = -1;
-    return;
-  }
+  const uint64_t groups = min((uint64_t)(all <= kFewCost * 256 ? 256 : ws.groups), (all + ws.least - 1) / ws.least);
+  // (workgroups go round the XCDs: these are as many on each, whatever their number)
+  const int per_xcd = ((int)groups + 7) / 8, me = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+  if (blockIdx.x == 0 && tid == 0) *ws.live = (int)groups;
+  if ((int)(blockIdx.x / 8) >= per_xcd || me >= (int)groups) return;
   uint64_t at = uniform(all * me / groups);
   const uint64_t end = uniform(all * (me + 1) / groups);
   const int share = uniform((int)min(all / groups, (uint64_t)(1 << 30)));
@@ -725,9 +729,10 @@ template <bool BF16, int DP, int BM>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, AttentionSpace ws) {
   const int w = blockIdx.x, tid = threadIdx.x, G = p.q_heads / p.kv_heads;
   const Owner u = ws.owner[w];
+  const int live = *ws.live;
   constexpr int PER = DP / 4;   // threads of a row
   const int m = blockIdx.y * join_rows(DP) + tid / PER, e = tid % PER * 4, mm = u.block * BM + m;
-  if (u.q < 0 || m >= u.rows || e >= p.head_dim) return;
+  if (w >= live || u.q < 0 || m >= u.rows || e >= p.head_dim) return;
   f32x4 o = {0, 0, 0, 0};
   float top = kLowest, l = 0;
   // eight parts' loads at a time: one after the other they wait for each other's latency
@@ -841,17 +846,20 @@ static AttentionPlan plan_attention(int M, int q_heads, int kv_heads, int head_d
   return a;
 }
 
+static int64_t owner_bytes(int groups) { return ((int64_t)groups * sizeof(Owner) + 16 + 255) & ~(int64_t)255; }
+
 int64_t attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim, bool bf16) {
   const AttentionPlan a = plan_attention(M, q_heads, kv_heads, head_dim, bf16);
-  return (int64_t)a.groups * sizeof(Owner) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
+  return a.groups == 0 ? 0 : owner_bytes(a.groups) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
 }
 
 template <bool BF16, int DP, int MQ, int WK>
 static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
   typedef AttentionShape<BF16, DP, MQ, WK> S;
   AttentionSpace ws;
-  ws.owner = static_cast<Owner*>(job.workspace);
-  ws.part = reinterpret_cast<float*>(ws.owner + plan.groups);
+  ws.live = static_cast<int*>(job.workspace);
+  ws.owner = reinterpret_cast<Owner*>(ws.live + 4);
+  ws.part = reinterpret_cast<float*>(static_cast<uint8_t*>(job.workspace) + owner_bytes(plan.groups));
   ws.groups = plan.groups;
   ws.least = plan.least;
   const size_t smem = S::LDS + 2 * (((size_t)job.M + 8) & ~(size_t)7) * sizeof(uint16_t);
