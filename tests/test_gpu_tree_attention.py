@@ -4,7 +4,8 @@ import pytest
 import torch
 
 from paper_2404_19124_amd import binding as B
-from tests.rows_common import check_attention, dev, exact_float, random_parents, random_table
+from oracle import rows_oracle as RO
+from tests.rows_common import attention_bound, check_attention, dev, exact_float, random_parents, random_table
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -241,3 +242,46 @@ def test_the_same_call_twice_gives_the_same_bits():
     first = c.run()
     for _ in range(3):
         assert torch.equal(c.run(), first)
+
+
+def seen_by(parent, row):
+    rows = [0]
+    while row > 0 and len(rows) <= 8:
+        rows.append(row)
+        row = parent[row - 1] + 1
+    return rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,KH,D,M,ctx", [(2, 2, 64, 9, [5, 0, 40]), (2, 1, 128, 7, [2000, 61]), (8, 2, 128, 20, [300, 3]), (4, 1, 80, 70, [50, 130]),
+                                          (8, 1, 128, 30, [700, 64]), (2, 2, 256, 6, [20, 100]), (4, 2, 192, 60, [90])])
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(H, KH, D, M, ctx, dtype):
+    """Infinities and NaN in a node's values reach the node and those below it, in their elements, and nobody else; NaN in a
+    node's keys reaches the same rows whole."""
+    c = Case(H, KH, D, 16, M, ctx, dtype, seed=21)
+    args = c.oracle_args()
+    clean, weighted, products, n_keys = RO.attention(**args)
+    bound = attention_bound(clean, weighted, products, n_keys, D, dtype == "bf16")
+    marks = {2: (3, float("inf")), 4: (0, float("nan")), 5: (D - 1, float("-inf")), 1: (3, float("-inf"))}   # row: element, value
+    for row, (e, x) in marks.items():
+        c.v_new[:, row, KH - 1, e] = x
+    keys = M if M > 6 else 6
+    c.k_new[:, keys, 0, 1] = float("nan")
+    got = exact_float(c.run())
+    G = H // KH
+    for q in range(c.b):
+        for r in range(c.n_nodes[q] + 1):
+            seen = seen_by(c.parent[q], r)
+            for h in range(H):
+                want = clean[q, r, h].copy()
+                if h // G == KH - 1:
+                    for e in (0, 3, D - 1):
+                        bad = [x for row, (at, x) in marks.items() if at == e and row in seen]
+                        if bad:
+                            want[e] = sum(bad)
+                if h // G == 0 and keys in seen:
+                    want[:] = np.nan
+                fine = np.isfinite(want)
+                assert np.array_equal(want[~fine], got[q, r, h][~fine], equal_nan=True), (q, r, h)
+                off = np.abs(want[fine] - got[q, r, h][fine])
+                assert (off <= np.broadcast_to(bound[q, r, h], want.shape)[fine]).all(), (q, r, h)
