@@ -371,6 +371,115 @@ struct Segment {
   const uint8_t *k_cache, *k_rows;   // of the head
 };
 
+// This workgroup's tiles: an equal share of all, in the order sequence, group of heads, block, head, tile.  A group has as
+// many heads as a share holds units: the blocks of a head, which read the same keys, then run beside each other on one XCD
+// (consecutive shares do) and not one after the other in one workgroup.  Batch of 32, 8 key/value heads of 128, 384 query rows
+// a head in three blocks: 298 us with all tiles of a block before the next one's (940 MB from beyond the L2 for 385 MB of keys
+// and values) and no unit cost, 244 us so.
+template <int BM, int COST>
+struct Schedule {
+  const AttentionJob& p;
+  const int G;
+  uint64_t all, groups, at, end, start;   // cost of all; workgroups that share it; this one's places; where sequence q starts
+  uint64_t unit_end;                      // of the segment that is worked on
+  int me, share, q;
+
+  // false: this workgroup has no share
+  __device__ __forceinline__ bool live(const AttentionSpace& ws) {
+    const int lane = threadIdx.x & 63;
+    all = 0;
+    for (int q0 = 0; q0 < p.batch; q0 += 64) {
+      uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, COST).total : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
+      all += t;
+    }
+    all = uniform(all);
+    groups = min((uint64_t)(all <= kFewCost * 256 ? 256 : ws.groups), (all + ws.least - 1) / ws.least);
+    // (workgroups go round the XCDs: these are as many on each, whatever their number)
+    const int per_xcd = ((int)groups + 7) / 8;
+    me = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ws.live = (int)groups;
+    if ((int)(blockIdx.x / 8) >= per_xcd || me >= (int)groups) return false;
+    at = uniform(all * me / groups);
+    end = uniform(all * (me + 1) / groups);
+    share = uniform((int)min(all / groups, (uint64_t)(1 << 30)));
+    q = 0;
+    start = 0;
+    for (int q0 = 0;; q0 += 64) {
+      uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, COST).total : 0, sum = t;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint64_t y = __shfl_up((unsigned long long)sum, d);
+        if (lane >= d) sum += y;
+      }
+      const uint64_t over = __ballot(start + sum > at);
+      if (over) {
+        const int l = __ffsll((unsigned long long)over) - 1;
+        q = uniform(q0 + l);
+        start = uniform(start + (uint64_t)__shfl((unsigned long long)(sum - t), l));
+        return true;
+      }
+      start = uniform(start + (uint64_t)__shfl((unsigned long long)sum, 63));
+    }
+  }
+
+  __device__ __forceinline__ uint64_t of_sequence(Segment& s, int seq) const {
+    const SeqTiles t = seq_tiles<true>(p, seq, BM, COST);
+    s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
+    s.heads = uniform(min(max(share / (t.tiles + COST), 1), p.kv_heads));
+    return t.total;
+  }
+  // the rest of a segment, `cost` of whose unit other workgroups bear, from place `from` on; false: there is no tile in it
+  __device__ __forceinline__ bool finish(Segment& s, uint64_t from, int cost) const {
+    const int upto = cost + (int)min(end - from, (uint64_t)(s.tiles + COST - cost));
+    s.tile0 = max(cost - COST, 0);
+    s.n_seg = max(upto - COST, 0) - s.tile0;
+    s.keys = s.ctx + min(s.nodes, (s.block * BM + BM - 1) / G) + 1;
+    s.n_tiles = max(min(s.n_seg, (s.keys + KT - 1) / KT - s.tile0), 1);   // (tiles behind that hold rows that are nobody's ancestor)
+    s.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)s.g * p.cache_head;
+    s.k_rows = static_cast<const uint8_t*>(p.k_new) + s.q * p.new_seq + (int64_t)s.g * p.new_head;
+    return s.n_seg > 0;
+  }
+  // the segment behind s, the one that is worked on; false: there is none
+  __device__ __forceinline__ bool following(Segment& s) const {
+    if (unit_end >= end) return false;
+    if (s.g < s.last_head) {
+      ++s.g;
+    } else if (++s.block < s.blocks) {
+      s.g -= (s.g % s.heads);   // (groups start at multiples of their size)
+    } else {
+      s.block = 0;
+      if (++s.g == p.kv_heads) {
+        s.g = 0;
+        do ++s.q;
+        while (of_sequence(s, s.q) == 0);
+      }
+      s.last_head = min(s.g + s.heads, p.kv_heads) - 1;
+    }
+    return finish(s, unit_end, 0);
+  }
+  __device__ __forceinline__ void advance(const Segment& s) { unit_end += (uint64_t)(s.tiles + COST); }
+  __device__ __forceinline__ bool first(Segment& s) {
+    of_sequence(s, q);
+    const int span = s.tiles + COST;
+    const uint64_t unit = uniform((at - start) / (uint64_t)span);
+    const int cost = uniform((int)(at - start - unit * (uint64_t)span));
+    const int per = s.heads * s.blocks, group = uniform((int)(unit / (uint64_t)per)), in = uniform((int)(unit - (uint64_t)group * (uint64_t)per));
+    s.last_head = min((group + 1) * s.heads, p.kv_heads) - 1;
+    const int size = s.last_head + 1 - group * s.heads;
+    s.block = uniform(in / size);
+    s.g = uniform(group * s.heads + in - s.block * size);
+    unit_end = at + (uint64_t)(span - cost);
+    if (finish(s, at, cost)) return true;
+    if (!following(s)) return false;   // (nothing but the cost of its queries)
+    advance(s);
+    return true;
+  }
+  // the workgroup that takes the last tile of the segment's unit
+  __device__ __forceinline__ int last() const { return (int)((unit_end * groups - 1) / all); }
+};
+
 // How a workgroup copies tiles into LDS, one ahead of the one it works on, across its segments.  A wave copies a fourth of a
 // tile's rows, 1 KiB (RPI rows) per instruction.  Where the wave's 16 tokens lie in one page, their place is one address for all
 // lanes, and the lanes' offsets from it are the same for every tile: it is found for 64 tiles at once, a tile per lane.
@@ -510,111 +619,23 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   typedef AttentionShape<BF16, DP, MQ, WK> S;
   typedef AttentionTile<BF16, DP, MQ, WK> Tile;
   typedef TileCopy<BF16, DP, MQ, WK> Copy;
-  constexpr int ESZ = S::ESZ, BM = S::BM, kUnitCost = unit_cost(BF16);
+  constexpr int ESZ = S::ESZ, BM = S::BM;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   __shared__ uint32_t s_valid[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
   const int wq = wave / WK, wk = wave % WK;
   const int G = p.q_heads / p.kv_heads;
 
-  // ---- this workgroup's tiles: an equal share of all, in the order sequence, group of heads, block, head, tile.  A group has as
-  // many heads as a share holds units: the blocks of a head, which read the same keys, then run beside each other on one XCD
-  // (consecutive shares do) and not one after the other in one workgroup.  Batch of 32, 8 key/value heads of 128, 384 query rows
-  // a head in three blocks: 298 us with all tiles of a block before the next one's (940 MB from beyond the L2 for 385 MB of keys
-  // and values) and no unit cost, 244 us so ----
-  uint64_t all = 0;
-  for (int q0 = 0; q0 < p.batch; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, kUnitCost).total : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
-    all += t;
-  }
-  all = uniform(all);
-  const uint64_t groups = min((uint64_t)(all <= kFewCost * 256 ? 256 : ws.groups), (all + ws.least - 1) / ws.least);
-  // (workgroups go round the XCDs: these are as many on each, whatever their number)
-  const int per_xcd = ((int)groups + 7) / 8, me = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
-  if (blockIdx.x == 0 && tid == 0) *ws.live = (int)groups;
-  if ((int)(blockIdx.x / 8) >= per_xcd || me >= (int)groups) return;
-  uint64_t at = uniform(all * me / groups);
-  const uint64_t end = uniform(all * (me + 1) / groups);
-  const int share = uniform((int)min(all / groups, (uint64_t)(1 << 30)));
-  int q = 0;
-  uint64_t start = 0;   // of sequence q
-  for (int q0 = 0;; q0 += 64) {
-    uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, kUnitCost).total : 0, sum = t;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint64_t y = __shfl_up((unsigned long long)sum, d);
-      if (lane >= d) sum += y;
-    }
-    const uint64_t over = __ballot(start + sum > at);
-    if (over) {
-      const int l = __ffsll((unsigned long long)over) - 1;
-      q = uniform(q0 + l);
-      start = uniform(start + (uint64_t)__shfl((unsigned long long)(sum - t), l));
-      break;
-    }
-    start = uniform(start + (uint64_t)__shfl((unsigned long long)sum, 63));
-  }
-  Owner mine = {-1, 0, 0, 0, 0};
-
-  // ---- segments ----
-  auto of_sequence = [&](Segment& s, int seq) {
-    const SeqTiles t = seq_tiles<true>(p, seq, BM, kUnitCost);
-    s.q = seq, s.ctx = t.ctx, s.nodes = t.nodes, s.tiles = t.tiles, s.blocks = t.blocks;
-    s.heads = uniform(min(max(share / (t.tiles + kUnitCost), 1), p.kv_heads));
-    return t.total;
-  };
-  // the rest of a segment, `cost` of whose unit other workgroups bear, from place `from` on; false: there is no tile in it
-  auto finish = [&](Segment& s, uint64_t from, int cost) {
-    const int upto = cost + (int)min(end - from, (uint64_t)(s.tiles + kUnitCost - cost));
-    s.tile0 = max(cost - kUnitCost, 0);
-    s.n_seg = max(upto - kUnitCost, 0) - s.tile0;
-    s.keys = s.ctx + min(s.nodes, (s.block * BM + BM - 1) / G) + 1;
-    s.n_tiles = max(min(s.n_seg, (s.keys + KT - 1) / KT - s.tile0), 1);   // (tiles behind that hold rows that are nobody's ancestor)
-    s.k_cache = static_cast<const uint8_t*>(p.k) + (int64_t)s.g * p.cache_head;
-    s.k_rows = static_cast<const uint8_t*>(p.k_new) + s.q * p.new_seq + (int64_t)s.g * p.new_head;
-    return s.n_seg > 0;
-  };
-  // the segment behind s, whose unit starts at place `from`; false: there is none
-  auto following = [&](Segment& s, uint64_t from) {
-    if (from >= end) return false;
-    if (s.g < s.last_head) {
-      ++s.g;
-    } else if (++s.block < s.blocks) {
-      s.g -= (s.g % s.heads);   // (groups start at multiples of their size)
-    } else {
-      s.block = 0;
-      if (++s.g == p.kv_heads) {
-        s.g = 0;
-        do ++s.q;
-        while (of_sequence(s, s.q) == 0);
-      }
-      s.last_head = min(s.g + s.heads, p.kv_heads) - 1;
-    }
-    return finish(s, from, 0);
-  };
+  Schedule<BM, unit_cost(BF16)> plan = {p, G};
+  if (!plan.live(ws)) return;
   Segment now;
-  of_sequence(now, q);
-  uint64_t unit_end;   // of the segment that is worked on
-  bool more;
-  {
-    const int span = now.tiles + kUnitCost;
-    const uint64_t unit = uniform((at - start) / (uint64_t)span);
-    const int cost = uniform((int)(at - start - unit * (uint64_t)span));
-    const int per = now.heads * now.blocks, group = uniform((int)(unit / (uint64_t)per)), in = uniform((int)(unit - (uint64_t)group * (uint64_t)per));
-    now.last_head = min((group + 1) * now.heads, p.kv_heads) - 1;
-    const int size = now.last_head + 1 - group * now.heads;
-    now.block = uniform(in / size);
-    now.g = uniform(group * now.heads + in - now.block * size);
-    unit_end = at + (uint64_t)(span - cost);
-    more = finish(now, at, cost);
-    if (!more && (more = following(now, unit_end))) unit_end += (uint64_t)(now.tiles + kUnitCost);   // (nothing but the cost of its queries)
-  }
+  Owner mine = {-1, 0, 0, 0, 0};
+  bool more = plan.first(now);
   if (!more) {
-    if (tid == 0) ws.owner[me] = mine;
+    if (tid == 0) ws.owner[plan.me] = mine;
     return;
   }
+  const int me = plan.me;
 
   // a negative scale goes into the queries' sign, a scale of zero makes them zero: the largest product has the largest weight
   const float q_sign = p.scale < 0 ? -1.0f : p.scale == 0 ? 0.0f : 1.0f;
@@ -629,7 +650,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
   while (more) {
     Segment next = now;
-    more = following(next, unit_end);
+    more = plan.following(next);
     const int rows = (now.nodes + 1) * G - now.block * BM;                     // query rows from this unit's first on
     // ---- parents' rows, where tiles hold rows (two sets: others may still be at the last segment) ----
     uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + S::LDS) + (n_units & 1) * ((p.M + 8) & ~7);
@@ -726,7 +747,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     // ---- out, or what has been summed so far ----
     const bool whole = now.n_seg == now.tiles;
     if (!whole && now.tile0 == 0)   // the unit ends in the workgroup that takes its last tile
-      mine = {now.q, now.g, now.block, (int)((unit_end * groups - 1) / all), min(rows, BM)};
+      mine = {now.q, now.g, now.block, plan.last(), min(rows, BM)};
     // A weight of zero does not take out a value that is not finite of a row that some of these rows do not see: sums that are not
     // finite are found once more, from the keys that each row sees.  (Taking them out of every tile with rows of the tree ahead of
     // the product, where there are any: 41 -> 46 us for 64 sequences of 100 tokens)
@@ -783,7 +804,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         }
       }
     }
-    unit_end += (uint64_t)(next.tiles + kUnitCost);
+    plan.advance(next);
     now = next;
     f = f_next;
     ++n_units;
@@ -832,73 +853,146 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, Att
   else *reinterpret_cast<f32x4*>(to + e * 4) = o;
 }
 
-// float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): one workgroup per
-// (row, query head, sequence), whose four waves take every fourth key, four elements of a row per lane, with
-// the running maximum and sum of the softmax, and are joined at the end.
-__global__ __launch_bounds__(256) void attention_f32_kernel(AttentionJob p) {
-  __shared__ float s_m[4], s_l[4], s_o[4][256];
-  __shared__ int s_row[kMaxStages + 1], s_rows;
-  const int r = blockIdx.x, h = blockIdx.y, q = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nodes = p.n_nodes ? min(max(p.n_nodes[q], -1), p.M) : p.M;
-  if (r > nodes) return;
-  const int g = h / (p.q_heads / p.kv_heads), ctx = min(max(p.ctx_len[q], 0), p.max_blocks * p.block_size);
-  if (tid == 0) {
-    int n = 0;
-    for (int node = r - 1; node >= 0 && n < kMaxStages;) {
-      s_row[n++] = node + 1;
-      const int up = p.node_parent[(int64_t)q * p.M + node];
-      node = up < node ? up : -1;
+// float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): units of 16 query
+// rows, four to a wave, straight from memory.  16 lanes take a key, four keys at once, 16 elements of the head per lane; the
+// waves read the same keys, three of them from the cache.  Bound by the vector units: 70 instructions for a key and a row.
+constexpr int kWideRows = 16;   // query rows of a unit
+__global__ __launch_bounds__(256, 2) void attention_wide_kernel(AttentionJob p, AttentionSpace ws) {
+  constexpr int BM = kWideRows, DP = 256;
+  const int G = p.q_heads / p.kv_heads, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, grp = lane >> 4;
+  Schedule<BM, unit_cost(false)> plan = {p, G};
+  if (!plan.live(ws)) return;
+  Segment now;
+  Owner mine = {-1, 0, 0, 0, 0};
+  bool more = plan.first(now);
+  const float sc = p.scale * kLog2e;
+  while (more) {
+    const int rows = (now.nodes + 1) * G - now.block * BM;
+    f32x4 x[4][4], o[4][4];
+    float m[4], l[4];
+    int row_of[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int mm = wave * 4 + i < rows ? now.block * BM + wave * 4 + i : now.block * BM;
+      row_of[i] = mm / G;
+      const float* from = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.q) + now.q * p.q_seq + (int64_t)row_of[i] * p.q_row +
+                                                         (int64_t)(now.g * G + mm % G) * p.q_head);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int e = c * 64 + l16 * 4;
+        x[i][c] = e < p.head_dim && p.scale != 0 ? *reinterpret_cast<const f32x4*>(from + e) : (f32x4){0, 0, 0, 0};
+        o[i][c] = (f32x4){0, 0, 0, 0};
+      }
+      m[i] = kLowest, l[i] = 0;
     }
-    s_row[n++] = 0;
-    s_rows = n;
-  }
-  __syncthreads();
-  const float* qr = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.q) + q * p.q_seq + r * p.q_row + h * p.q_head);
-  float x[4], o[4] = {0, 0, 0, 0}, m = kLowest, l = 0;
+    const int64_t to_v_cache = static_cast<const uint8_t*>(p.v) - static_cast<const uint8_t*>(p.k);
+    const int64_t to_v_rows = static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new);
+    auto load = [&](const uint8_t* at, f32x4 (&y)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = lane + i * 64 < p.head_dim ? qr[lane + i * 64] * p.scale : 0.0f;
-  const int keys = ctx + s_rows;
-  for (int t = wave; t < keys; t += 4) {
-    const float *k, *v;
-    if (t < ctx) {
-      const int b = p.block_table[(int64_t)q * p.max_blocks + t / p.block_size];
-      if (b < 0 || b >= p.n_blocks) continue;
-      const int64_t at = b * p.block + t % p.block_size * p.slot + g * p.cache_head;
-      k = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.k) + at);
-      v = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.v) + at);
-    } else {
-      const int64_t at = q * p.new_seq + s_row[t - ctx] * p.new_row + g * p.new_head;
-      k = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.k_new) + at);
-      v = reinterpret_cast<const float*>(static_cast<const uint8_t*>(p.v_new) + at);
+      for (int c = 0; c < 4; ++c) {
+        const int e = c * 64 + l16 * 4;
+        y[c] = e < p.head_dim ? *reinterpret_cast<const f32x4*>(at + e * 4) : (f32x4){0, 0, 0, 0};
+      }
+    };
+    auto take = [&](const f32x4 (&k)[4], const f32x4 (&v)[4], uint32_t sees) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 d = x[i][0] * k[0];
+#pragma unroll
+        for (int c = 1; c < 4; ++c) d += x[i][c] * k[c];
+        const float score = row16_sum((d[0] + d[1]) + (d[2] + d[3])) * sc;
+        if ((sees >> i) & 1) {
+          if (score > m[i] + kSlack) {
+            const float keep = __builtin_amdgcn_exp2f(m[i] - score);
+            m[i] = score;
+            l[i] *= keep;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[i][c] *= keep;
+          }
+          const float w = __builtin_amdgcn_exp2f(score - m[i]);
+          l[i] += w;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[i][c] += w * v[c];
+        }
+      }
+    };
+    // ---- cached tokens: the next key's loads are sent before one is worked on ----
+    const int from = now.tile0 * KT, to = min((now.tile0 + now.n_tiles) * KT, now.keys), cached = min(to, now.ctx);
+    auto place = [&](int key) -> const uint8_t* {   // NULL: takes no part
+      if (key >= cached) return nullptr;
+      const int b = key / p.block_size, t = p.block_table[(int64_t)now.q * p.max_blocks + b];
+      return t >= 0 && t < p.n_blocks ? now.k_cache + t * p.block + (key - b * p.block_size) * p.slot : nullptr;
+    };
+    f32x4 k[4], v[4];
+    const uint8_t* at = place(from + grp);
+    if (at) load(at, k), load(at + to_v_cache, v);
+    for (int t = from; t < cached; t += 4) {
+      const uint8_t* next = place(t + 4 + grp);
+      f32x4 k2[4], v2[4];
+      if (next) load(next, k2), load(next + to_v_cache, v2);
+      if (at) take(k, v, 15);
+      at = next;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) k[c] = k2[c], v[c] = v2[c];
     }
-    float s = 0;
+    // ---- rows of the tree ----
+    for (int t = max(from, now.ctx); t < to; t += 4) {
+      const int r = t + grp - now.ctx;
+      uint32_t sees = 0;
+      if (t + grp < to) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + i * 64 < p.head_dim) s += x[i] * k[lane + i * 64];
-    s = wave_sum(s);
-    const float top = fmaxf(m, s), w = expf(s - top), keep = expf(m - top);
-    l = l * keep + w;
+        for (int i = 0; i < 4; ++i) {
+          int row = row_of[i];
+          for (int n = 0; n < kMaxStages && row > r; ++n) {
+            const int up = p.node_parent[(int64_t)now.q * p.M + row - 1];
+            row = n + 1 < kMaxStages && up >= 0 && up < row - 1 ? up + 1 : 0;
+          }
+          if (row == r) sees |= 1u << i;
+        }
+      }
+      if (sees) {
+        load(now.k_rows + (int64_t)r * p.new_row, k);
+        load(now.k_rows + to_v_rows + (int64_t)r * p.new_row, v);
+        take(k, v, sees);
+      }
+    }
+    // ---- join of the four keys' lanes; lane group i writes row i ----
+    const bool whole = now.n_seg == now.tiles;
+    if (!whole && now.tile0 == 0) mine = {now.q, now.g, now.block, plan.last(), min(rows, BM)};
+    f32x4 y[4];
+    float top = 0, sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + i * 64 < p.head_dim) o[i] = o[i] * keep + w * v[lane + i * 64];
-    m = top;
-  }
-  if (lane == 0) s_m[wave] = m, s_l[wave] = l;
+    for (int i = 0; i < 4; ++i) {
+      const float all_m = groups_max(m[i]), f = __builtin_amdgcn_exp2f(m[i] - all_m), all_l = groups_sum(l[i] * f);
+      if (grp == i) top = all_m, sum = all_l;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s_o[wave][lane + i * 64] = o[i];
-  __syncthreads();
-  // (row 0 is always there: one of the four has a key)
-  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float sum = 0, val = 0;
-  for (int w = 0; w < 4; ++w) {
-    const float f = expf(s_m[w] - top);
-    sum += f * s_l[w];
-    val += f * s_o[w][tid];
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float s = groups_sum(f > 0 ? o[i][c][j] * f : 0.0f);
+          if (grp == i) y[c][j] = s;
+        }
+    }
+    const int r = wave * 4 + grp;
+    if (r < rows) {
+      const int mm = now.block * BM + r;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int e = c * 64 + l16 * 4;
+        if (e < p.head_dim) {
+          if (whole) *reinterpret_cast<f32x4*>(static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)(mm / G) * p.out_row + (int64_t)(now.g * G + mm % G) * p.out_head + e * 4) = y[c] * (1.0f / sum);
+          else *reinterpret_cast<f32x4*>(ws.part + ((int64_t)(plan.me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + r) * (DP + 4) + e) = y[c];
+        }
+      }
+      if (!whole && l16 == 0) {
+        float* part = ws.part + ((int64_t)(plan.me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + r) * (DP + 4);
+        part[DP] = top, part[DP + 1] = sum;
+      }
+    }
+    more = plan.following(now);
+    if (more) plan.advance(now);
   }
-  if (tid < p.head_dim) {
-    uint8_t* to = static_cast<uint8_t*>(p.out) + q * p.out_seq + r * p.out_row + h * p.out_head;
-    reinterpret_cast<float*>(to)[tid] = val / sum;
-  }
+  if (tid == 0) ws.owner[plan.me] = mine;
 }
 
 // Query rows of a key/value head: at most 16, the waves share the keys; at most 32, by twos; more, each has rows of its own.
@@ -911,7 +1005,7 @@ static AttentionPlan plan_attention(int M, int q_heads, int kv_heads, int head_d
   const int64_t rows = (int64_t)(M + 1) * (q_heads / kv_heads);
   a.bm = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || a.dp == 256 || !bf16 ? 64 : 128;
   a.groups = a.dp * (bf16 ? 1 : 2) <= 128 ? 512 : 256;   // two workgroups of 64 KiB fit a CU
-  if (!bf16 && a.dp == 256) a.groups = 0;
+  if (!bf16 && a.dp == 256) a.bm = kWideRows, a.groups = 512;
   a.least = 2;
   return a;
 }
@@ -920,18 +1014,23 @@ static int64_t owner_bytes(int groups) { return ((int64_t)groups * sizeof(Owner)
 
 int64_t attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim, bool bf16) {
   const AttentionPlan a = plan_attention(M, q_heads, kv_heads, head_dim, bf16);
-  return a.groups == 0 ? 0 : owner_bytes(a.groups) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
+  return owner_bytes(a.groups) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
 }
 
-template <bool BF16, int DP, int MQ, int WK>
-static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
-  typedef AttentionShape<BF16, DP, MQ, WK> S;
+static AttentionSpace space_of(const AttentionJob& job, const AttentionPlan& plan) {
   AttentionSpace ws;
   ws.live = static_cast<int*>(job.workspace);
   ws.owner = reinterpret_cast<Owner*>(ws.live + 4);
   ws.part = reinterpret_cast<float*>(static_cast<uint8_t*>(job.workspace) + owner_bytes(plan.groups));
   ws.groups = plan.groups;
   ws.least = plan.least;
+  return ws;
+}
+
+template <bool BF16, int DP, int MQ, int WK>
+static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
+  const AttentionSpace ws = space_of(job, plan);
   const size_t smem = S::LDS + 2 * (((size_t)job.M + 8) & ~(size_t)7) * sizeof(uint16_t);
   int device = 0;
   hipError_t e = hipGetDevice(&device);
@@ -952,8 +1051,12 @@ static hipError_t launch_attention_t(const AttentionJob& job, const AttentionPla
 
 hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st) {
   const AttentionPlan a = plan_attention(job.M, job.q_heads, job.kv_heads, job.head_dim, bf16);
-  if (a.groups == 0) {
-    hipLaunchKernelGGL(attention_f32_kernel, dim3(job.M + 1, job.q_heads, job.batch), dim3(256), 0, st, job);
+  if (!bf16 && a.dp == 256) {
+    const AttentionSpace ws = space_of(job, a);
+    hipLaunchKernelGGL(attention_wide_kernel, dim3(a.groups), dim3(256), 0, st, job, ws);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attention_join_kernel<false, 256, kWideRows>), dim3(a.groups, kWideRows / join_rows(256)), dim3(256), 0, st, job, ws);
     return hipGetLastError();
   }
 #define LAUNCH(BF16, DP, BM, MQ, WK) \
