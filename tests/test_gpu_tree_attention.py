@@ -285,3 +285,55 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(H, KH, D, M, ctx, dt
                 assert np.array_equal(want[~fine], got[q, r, h][~fine], equal_nan=True), (q, r, h)
                 off = np.abs(want[fine] - got[q, r, h][fine])
                 assert (off <= np.broadcast_to(bound[q, r, h], want.shape)[fine]).all(), (q, r, h)
+
+
+WIDE = {
+    "split_over_workgroups": dict(H=8, KH=1, D=160, page=7, M=40, ctx=[3000, 0, 200]),
+    "one_token": dict(H=3, KH=3, D=132, page=16, M=0, ctx=[1, 500, 64, 0]),
+    "grouped": dict(H=16, KH=2, D=256, page=64, M=20, ctx=[1000, 70, 129]),
+    "many_nodes": dict(H=2, KH=2, D=200, page=16, M=300, ctx=[90]),
+    "idle": dict(H=5, KH=1, D=144, page=32, M=9, ctx=[40, 300, 0], n_nodes=[9, -1, 0]),
+    "loud": dict(H=4, KH=4, D=256, page=16, M=12, ctx=[200, 31], loud=12.0),
+}
+
+
+@pytest.mark.parametrize("name", WIDE)
+def test_wide_float32_heads(name):
+    c = Case(dtype="f32", seed=40 + len(name), **WIDE[name])
+    c.check(c.run())
+    if c.ctx[0] > 2 * c.page:      # blocks that are not there, and parents that are not before their node
+        c.table[0, 1], c.table[0, 2] = -1, c.k.shape[0]
+        if c.M > 8:
+            c.parent[0, 5], c.parent[0, 8] = 7, 2 ** 31 - 1
+        c.check(c.run())
+
+
+def test_wide_float32_heads_captured_and_replayed():
+    c = Case(H=6, KH=2, D=192, page=16, M=11, ctx=[700, 33, 0], dtype="f32", seed=51)
+    out = torch.full(c.q.shape, 7.0, device="cuda")
+    ctx, count = dev(c.ctx), dev(c.n_nodes)
+    a = dict(q=c.q, k_new=c.k_new, v_new=c.v_new, k_cache=c.k, v_cache=c.v, block_table=dev(c.table), ctx_len=ctx, node_parent=dev(c.parent),
+             n_nodes=count, out=out, workspace=c.workspace(), scale=-c.scale)
+    c.scale = -c.scale
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        B.spec_tree_attention(**a)
+    for lengths, nodes in (([700, 33, 0], [11, 10, 9]), ([1, 20, 0], [0, -1, 11]), ([600, 0, 0], [11, 11, 0])):
+        c.ctx, c.n_nodes = np.array(lengths, np.int32), np.array(nodes, np.int32)
+        ctx.copy_(dev(c.ctx))
+        count.copy_(dev(c.n_nodes))
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_shares_that_hold_several_heads(dtype):
+    """So many short sequences that a share is several heads' units, in groups of heads that do not divide their number, each of
+    several blocks of query rows; some sequences take no part."""
+    n_nodes = [-1 if q % 11 == 3 else 8 - q % 4 for q in range(128)]
+    c = Case(H=160, KH=5, D=16, page=16, M=8, ctx=[(37 * q) % 150 for q in range(128)], dtype=dtype, seed=61, n_nodes=n_nodes)
+    c.check(c.run())
