@@ -317,7 +317,7 @@ struct AttentionTile {
 // One turn of a workgroup: tile `cur` has landed; the next one is copied into `other` while it is worked on.
 template <bool BF16, int DP, int MQ, int WK, typename Copy>
 __device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& x, lds_u8* __restrict cur, lds_u8* __restrict other, const uint32_t* valid,
-                                               int t0, int ctx, const uint16_t* s_up, float sc, Copy&& copy_next) {
+                                               int t0, int ctx, const uint16_t* s_up, float sc, bool active, Copy&& copy_next) {
   // this wave's copies have landed, and behind the barrier the others'; all are done with the other buffer
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
   __syncthreads();
@@ -325,7 +325,7 @@ __device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& 
   uint64_t cached = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) cached |= (uint64_t)valid[w] << (w * (KT / 4));
-  x.step(cur, cur + KT * AttentionShape<BF16, DP, MQ, WK>::ROWB, cached, t0, ctx, s_up, sc);
+  if (active) x.step(cur, cur + KT * AttentionShape<BF16, DP, MQ, WK>::ROWB, cached, t0, ctx, s_up, sc);
 }
 
 // One query row of one head over the keys [from, to), key by key, by one wave: four elements of the head per lane.
@@ -700,11 +700,12 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     if (now.n_tiles > 1) up = copy.source(now, 1, f);
     else up = first;
 
+    const bool active = uniform(wq) * MQ * 16 < rows;   // (of a unit with few rows only the first waves have any: the others just copy)
     // ---- tiles.  The next one is copied into the other buffer while one is worked on; the two buffers are distinct objects to
     // the compiler (restrict), so that a read of one does not wait for the copies into the other ----
     auto tile = [&](lds_u8* cur, lds_u8* other, int t) {
       attention_turn<BF16, DP, MQ, WK>(
-          x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, [&](lds_u8* to) {
+          x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, active, [&](lds_u8* to) {
             if (up.k_cache) copy.copy(up, to, s_valid[(turn + 1) & 1]);
           });
       if (t + 2 < now.n_tiles) up = copy.source(now, t + 2, f);
