@@ -9,7 +9,7 @@
 //
 // Bound by reading the keys and values where a key/value head has few query rows, by the vector and matrix units where it has many,
 // by latency in small calls: 64 sequences of one token over 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 sequences
-// of 46 rows over 2000 (32 heads) 219 us, 4.7 TB/s; 32 of 368 query rows over 4000 (8 heads) 215 us, 550 TFLOP/s; one of 46
+// of 46 rows over 2000 (32 heads) 218 us, 4.7 TB/s; 32 of 368 query rows over 4000 (8 heads) 206 us, 580 TFLOP/s; one of 46
 // rows over 600 (32 heads) 15.8 us.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
 // row's scores: the softmax, and the rescaling of the transposed sums, need no exchange but two swaps.  Weights are rounded to
 // bfloat16 for the second product (off by at most 2^-8 of themselves), their sum is not.
