@@ -12,7 +12,7 @@
 namespace specdraft {
 
 constexpr int row_chunks(bool out) { return out ? 1 : 2; }   // chunks of 8 tokens that a thread has in flight
-constexpr int kWideRows = 512;   // rows of which two fit a CU: 1024 threads each (46 rows of 32000: 12.7 us, with 512: 15.4 us)
+constexpr int kWideRows = 512;   // rows of which two fit a CU: 1024 threads each (34 rows of 32000: 12.7 us, with 512: 15.4 us)
 
 // eight neighbours; rows of an odd length start anywhere, so their words are not aligned to 16 bytes (the compiler's memcpy is one
 // 16-byte load all the same)
@@ -50,7 +50,7 @@ __device__ __forceinline__ float penalized(float v, int c, bool bit, float bias,
 // trip ahead.  The touched ones are left out there (their logits stay as they are): every wave lists their chunks, logits and all,
 // and works 64 of them off at a time.  Consecutive rows run on one XCD, in whose L2 their sequence's counts stay, and the logits
 // go past it: 2000 counts lie in half of a row's lines.
-// Bound by reading the logits: 32 sequences of 46 rows of 128256 bf16 logits, 2000 tokens emitted, 379 MB in 116 us (3.3 TB/s;
+// Bound by reading the logits: 32 sequences of 45 rows of 128256 bf16 logits, 2000 tokens emitted, 379 MB in 116 us (3.3 TB/s;
 // torch's largest sum reads 4.0 TB/s).  One element after the other: 603 us; touched tokens gathered again at a row's end: 140 us;
 // rows dealt out over the XCDs one by one: 144 us.
 template <bool BF16, bool OUT, int NT>

@@ -8,9 +8,9 @@
 // maximum m', l and o are multiplied by exp(m - m')).
 //
 // Bound by reading the keys and values where a key/value head has few query rows, by the vector and matrix units where it has many,
-// by latency in small calls: 64 sequences of one token over 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 sequences
-// of 46 rows over 2000 (32 heads) 218 us, 4.7 TB/s; 32 of 368 query rows over 4000 (8 heads) 206 us, 580 TFLOP/s; one of 46
-// rows over 600 (32 heads) 15.8 us.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
+// by latency in small calls: 64 sequences of one token over up to 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 of 33
+// rows over up to 2000 (32 heads) 218 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 206 us, 580 TFLOP/s;
+// one of 34 rows over 600 (32 heads) 15.6 us.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
 // row's scores: the softmax, and the rescaling of the transposed sums, need no exchange but two swaps.  Weights are rounded to
 // bfloat16 for the second product (off by at most 2^-8 of themselves), their sum is not.
 #include <atomic>
@@ -63,7 +63,7 @@ typedef const __attribute__((address_space(4))) int32_t* scalar_i32;
 
 // The work is cut into equal shares by COST: a unit costs its tiles and kUnitCost more for its queries and results (a sequence
 // with nothing cached, 24 units of one tile in one share: that workgroup took a third longer than all others).  32 sequences of
-// 8 key/value heads with 368 query rows: 0: 298 us, 1: 240 us, 2: 221 us, 3: 233 us; float32 tiles take longer, and a cost of 1 is best.
+// 8 key/value heads with 360 query rows: 0: 298 us, 1: 240 us, 2: 221 us, 3: 233 us; float32 tiles take longer, and a cost of 1 is best.
 constexpr int unit_cost(bool bf16) { return bf16 ? 2 : 1; }
 
 struct SeqTiles {
@@ -380,7 +380,7 @@ struct Segment {
 
 // This workgroup's tiles: an equal share of all, in the order sequence, group of heads, block, head, tile.  A group has as
 // many heads as a share holds units: the blocks of a head, which read the same keys, then run beside each other on one XCD
-// (consecutive shares do) and not one after the other in one workgroup.  Batch of 32, 8 key/value heads of 128, 384 query rows
+// (consecutive shares do) and not one after the other in one workgroup.  Batch of 32, 8 key/value heads of 128, 360 query rows
 // a head in three blocks: 298 us with all tiles of a block before the next one's (940 MB from beyond the L2 for 385 MB of keys
 // and values) and no unit cost, 244 us so.
 template <int BM, int COST>
@@ -824,7 +824,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 }
 
 // Units that several workgroups took part in: workgroup (w, y) joins some query rows of the one that started in workgroup w of
-// the launch above, in the order of the keys.  One small call (32 heads of 58 query rows, 12 parts each) reads and writes as
+// the launch above, in the order of the keys.  One small call (32 heads of 34 query rows, 6 parts each) reads and writes as
 // much for its parts as for its keys and values: the rows are spread over as many workgroups as there are.
 constexpr int join_rows(int DP) { return 256 / (DP / 4); }
 template <bool BF16, int DP, int BM>
@@ -867,7 +867,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, Att
 // float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): units of 16 query
 // rows, four to a wave, straight from memory.  16 lanes take a key, four keys at once, 16 elements of the head per lane; the
 // waves read the same keys, three of them from the cache.  Bound by the latency of a key's loads, one key ahead, and the vector
-// units: 4 sequences of up to 1000 tokens, 32 query heads on 8 of 192, 46 rows: 323 us, 8.3 TFLOP/s; one of 20000 tokens, 8 query
+// units: 4 sequences of up to 1000 tokens, 32 query heads on 8 of 192, 32 rows: 323 us, 8.3 TFLOP/s; one of 20000 tokens, 8 query
 // heads on one of 256: 118 us.  (A workgroup per row, unsplit: 1.02 ms and 12.1 ms.)
 constexpr int kWideRows = 16;   // query rows of a unit
 __global__ __launch_bounds__(256, 2) void attention_wide_kernel(AttentionJob p, AttentionSpace ws) {
