@@ -312,7 +312,9 @@ typedef struct {
 /* TREE ATTENTION.  For every row r of sequence q and every query head h, with g = h / (q_heads / kv_heads):
  *     out[q][r][h] = sum_k softmax_k(scale * q[q][r][h] . key_k[g]) value_k[g]
  * over the ctx_len[q] cached tokens and the rows 0 (the last token), the ancestors of r, and r itself.
- *   dtype       spec_dtype_t of q, k_new, v_new, cache and out; products and sums in float32
+ *   dtype       spec_dtype_t of q, k_new, v_new, cache and out; scores, softmax and sums in float32.  SPEC_BF16: the weights are
+ *               rounded to bfloat16 for their product with the values, each by at most 2^-8 of itself, and their sum is that of
+ *               the rounded ones
  *   head_dim    multiple of 8 (SPEC_BF16) or 4 (SPEC_F32), <= 256;  q_heads a multiple of kv_heads
  *   q, out      rows of q_heads;  k_new, v_new  rows of kv_heads, the same strides for both
  *   block_table dev [batch, max_blocks] int32;  ctx_len dev [batch] int32, taken as within [0, max_blocks * block_size]

@@ -12,7 +12,8 @@
 // rows over up to 2000 (32 heads) 218 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 206 us, 580 TFLOP/s;
 // one of 34 rows over 600 (32 heads) 15.6 us.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
 // row's scores: the softmax, and the rescaling of the transposed sums, need no exchange but two swaps.  Weights are rounded to
-// bfloat16 for the second product (off by at most 2^-8 of themselves), their sum is not.
+// bfloat16 for the second product, each by at most 2^-8 of itself (a product in float32 has an eighth of the rate: 141 and 1153
+// TFLOP/s), and their sum is that of the rounded ones: an output is a mean of the values with weights that far from the exact ones.
 #include <atomic>
 #include <type_traits>
 
@@ -23,6 +24,7 @@
 namespace specdraft {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -247,9 +249,14 @@ struct AttentionTile {
         for (int i = 0; i < 4; ++i) {
           const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mq][nb][i], sc, -m_run[mq]));
           s[mq][nb][i] = w;
-          l_run[mq] += w;
+          if constexpr (!BF16) l_run[mq] += w;
         }
     }
+    // (the sum is that of the weights as they are multiplied: equal values come out as they are, whatever the rounding)
+    auto sum = [&](int mq, uint32_t pair) {
+      const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+      l_run[mq] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, l_run[mq], false);
+    };
 
     if constexpr (BF16) {
       if constexpr (NB == 1) {
@@ -258,6 +265,8 @@ struct AttentionTile {
         for (int mq = 0; mq < MQ; ++mq) {
           const uint32_t lo = f32_to_bf16_pair(s[mq][0][0], s[mq][0][1]), hi = f32_to_bf16_pair(s[mq][0][2], s[mq][0][3]);
           w[mq] = __builtin_bit_cast(i16x4, (uint64_t)hi << 32 | lo);
+          sum(mq, lo);
+          sum(mq, hi);
         }
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
@@ -276,6 +285,8 @@ struct AttentionTile {
             const f32x4 a = s[mq][2 * j], b = s[mq][2 * j + 1];
             const u32x4 raw = {f32_to_bf16_pair(a[0], a[1]), f32_to_bf16_pair(a[2], a[3]), f32_to_bf16_pair(b[0], b[1]), f32_to_bf16_pair(b[2], b[3])};
             w[mq][j] = __builtin_bit_cast(bf16x8, raw);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum(mq, raw[i]);
           }
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
