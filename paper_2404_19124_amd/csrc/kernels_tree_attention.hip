@@ -4,8 +4,8 @@
 //
 // A UNIT is BM query rows of one key/value head of one sequence: the rows of all query heads that share it, tree row by tree
 // row.  Its keys are the cached tokens and then the sequence's rows, in TILES of 64.  One pass over the tiles keeps, per
-// query row, the running maximum m, sum l of the softmax's weights and the weighted sum o of the values (with a larger
-// maximum m', l and o are multiplied by exp(m - m')).
+// query row, a bound m of the scores so far, the sum l of the softmax's weights exp(score - m) and the weighted sum o of the
+// values (with a larger bound m', l and o are multiplied by exp(m - m')).
 //
 // Bound by reading the keys and values where a key/value head has few query rows, by the vector and matrix units where it has many,
 // by latency in small calls: 64 sequences of one token over up to 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 of 33
@@ -34,6 +34,8 @@ typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int KT = 64;   // keys of a tile
+// How far above the largest score so far the bound is set when it has to move (powers of 2): scores that rise by less leave it where
+// it is.  No weight is above 1, so that the largest values' products stay finite, and the largest is 2^-8 at least.
 constexpr float kSlack = 8;
 
 // larger / sum of a value and those of the lanes 16 and 32 away: the same query row's other keys
@@ -215,7 +217,7 @@ struct AttentionTile {
       }
     };
 
-    // ---- softmax: weights relative to the running maximum ----
+    // ---- softmax: weights relative to a bound of the scores ----
 #pragma unroll
     for (int mq = 0; mq < MQ; ++mq) {
       float top = s[mq][0][0];
@@ -224,10 +226,9 @@ struct AttentionTile {
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[mq][nb][i]);
       top = groups_max(top) * sc;
-      // (weights may grow to 2^8 before the maximum they are relative to is moved: what is summed is float32, and rounding a weight
-      // to bfloat16 is relative.  Moving it with every larger product: 128 of a tile's 330 vector instructions)
-      if (__any(top > m_run[mq] + kSlack)) {
-        const float m_new = fmaxf(m_run[mq], top), keep = __builtin_amdgcn_exp2f(m_run[mq] - m_new);
+      // (moving it with every larger score: 128 of a tile's 330 vector instructions)
+      if (__any(top > m_run[mq])) {
+        const float m_new = fmaxf(m_run[mq], top + kSlack), keep = __builtin_amdgcn_exp2f(m_run[mq] - m_new);
         m_run[mq] = m_new;
         l_run[mq] *= keep;
 #pragma unroll
@@ -926,9 +927,9 @@ __global__ __launch_bounds__(256, 2) void attention_wide_kernel(AttentionJob p, 
         for (int c = 1; c < 4; ++c) d += x[i][c] * k[c];
         const float score = row16_sum((d[0] + d[1]) + (d[2] + d[3])) * sc;
         if ((sees >> i) & 1) {
-          if (score > m[i] + kSlack) {
-            const float keep = __builtin_amdgcn_exp2f(m[i] - score);
-            m[i] = score;
+          if (score > m[i]) {
+            const float keep = __builtin_amdgcn_exp2f(m[i] - (score + kSlack));
+            m[i] = score + kSlack;
             l[i] *= keep;
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[i][c] *= keep;

@@ -39,3 +39,26 @@ def test_weights_that_are_all_rounded_the_same_way_do_not_move_the_sum(H, KH, D,
     got = exact_float(c.run())
     for q in range(c.b):
         assert (got[q, :c.n_nodes[q] + 1] == 1.9921875).all(), q
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+@pytest.mark.parametrize("H,KH,M", [(1, 1, 0), (8, 2, 3), (4, 1, 40)])
+def test_the_largest_values_stay_finite(D, H, KH, M, dtype):
+    """A cached key of score 0 and, behind it, rows of score 3: means of values near the type's largest one.  A mean of two or more
+    of them is exact to the rounding of the sums (16 U32), of the weights (U16 twice) and of the output."""
+    c = Case(H, KH, D, 16, M, [1, 0, 1], dtype, seed=73, depth=1)
+    c.q[:], c.k[:], c.k_new[:] = 0, 0, 0
+    c.q[..., 0], c.k_new[:, :, :, 0] = 1, 3
+    c.scale = 1.0
+    sign = torch.where(torch.rand((D,), generator=torch.Generator().manual_seed(6)) < 0.5, -1.0, 1.0).to(c.dtype).cuda()
+    c.v[:], c.v_new[:] = 3.0e38 * sign, 2.0e38 * sign
+    got = exact_float(c.run())
+    a, b = exact_float(c.v[0, 0, 0]), exact_float(c.v_new[0, 0, 0])
+    for q in range(c.b):
+        for r in range(c.n_nodes[q] + 1):
+            seen = 1 + (r > 0)
+            w = np.exp(-3.0) * float(c.ctx[q])
+            want = (w * a + seen * b) / (w + seen)
+            lim = (32 * U32 + (3 * U16 if dtype == "bf16" else 0)) * np.abs(want) * 1.5
+            assert bool((np.abs(got[q, r] - want) <= lim).all()), (q, r)
