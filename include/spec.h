@@ -324,8 +324,8 @@ typedef struct {
  * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.
  * A cached token whose block is outside [0, n_blocks) takes no part.  Cache slots at and past ctx_len, and rows of k_new and v_new
  * behind the last node, may hold anything.
- * Infinities and NaN among the keys and values of a row reach the rows that see it and no others (a sum of infinities costs time:
- * the rows it may have reached are done once more, key by key).
+ * Infinities and NaN among the keys and values of a row reach the rows that see it and no others.  (They cost time: the workgroups
+ * whose shares of the keys hold one beside rows of a tree, absent blocks or heads that are not 64, 128 or 256 wide do them twice.)
  *   workspace   dev, 16-byte aligned, at least spec_tree_attention_workspace() bytes, contents of no meaning before
  *               and after; calls that may overlap in time, replays of graphs among them, need one each
  * Limits: M <= 4096, batch and q_heads <= 65535, max_blocks * block_size <= 2^30. */

@@ -326,10 +326,75 @@ struct AttentionTile {
   }
 };
 
-// One turn of a workgroup: tile `cur` has landed; the next one is copied into `other` while it is worked on.
+// What a careful pass has left out of its rows' sums: the values that are not finite of the rows of the tree that each sees, of those
+// that are keys of the segment (key ctx + row in [from, to)).  A weight is above zero, and times such a value that value, but where the
+// key is not finite: there the sum is NaN, be the weight zero or not a number itself.
+template <bool BF16, int DP, int MQ, int WK>
+__device__ __forceinline__ void add_left_out(AttentionTile<BF16, DP, MQ, WK>& x, const uint8_t* k_rows, int64_t to_v, int64_t stride, int ctx, int from, int to,
+                                             const uint16_t* s_up, int last_word) {
+  constexpr int ESZ = BF16 ? 2 : 4;
+  const int grp = (opaque_tid() & 63) >> 4;
+  auto finite = [](uint32_t bits) { return BF16 ? (bits & 0x7f80) != 0x7f80 && (bits & 0x7f800000) != 0x7f800000 : (bits & 0x7f800000) != 0x7f800000; };
+#pragma unroll
+  for (int mq = 0; mq < MQ; ++mq) {
+    int row = x.row_of[mq];
+    bool sees = true;
+#pragma unroll 1
+    for (int n = 0; n <= kMaxStages; ++n) {
+      const bool here = sees && ctx + row >= from && ctx + row < to;
+      const uint8_t *k = k_rows + row * stride, *v = k + to_v;
+      float w = 1;
+#pragma unroll 1
+      for (int word = 0; word <= last_word; ++word) {
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(k + word * 16);
+        if (!finite(raw[0]) || !finite(raw[1]) || !finite(raw[2]) || !finite(raw[3])) w = __builtin_nanf("");
+      }
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) {
+        const int e = d * 16 + grp * 4;
+        if (!here || e * ESZ > last_word * 16 + 15) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y = BF16 ? bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(v)[e + i]) : reinterpret_cast<const float*>(v)[e + i];
+          if (!(y * 0.0f == 0.0f)) x.o[mq][d][i] += w * y;
+        }
+      }
+      sees = sees && row > 0;
+      row = row > 0 && n + 1 < kMaxStages ? s_up[row] : 0;
+    }
+  }
+}
+
+// A weight of zero does not take out a value that is not finite, of a row of the tree that only some rows see, and a zero of a query
+// not what stands behind the elements of a key (copies of its last 16 bytes).  Where segments with such keys have sums that are
+// not finite, the workgroup goes through its share a second time, CAREFULLY: in every tile that has landed, zeros take the place of what
+// is behind the elements and of the values that are not finite of all that is not a cached token.  (In every pass over a tile with rows
+// of the tree: 41 -> 46 us for 64 sequences of 100 tokens.)
+template <bool BF16, int DP, int MQ, int WK>
+__device__ __forceinline__ void clean_tile(lds_u8* cur, uint64_t cached, int last_word) {
+  typedef AttentionShape<BF16, DP, MQ, WK> S;
+  constexpr uint32_t kExponent = BF16 ? 0x7f80 : 0x7f800000;
+  for (int i = opaque_tid(); i < KT * S::CH; i += 256) {
+    const int key = i / S::CH, word = (i % S::CH) ^ (key & S::SWZ);
+    if (word > last_word) *reinterpret_cast<lds_u32x4*>(cur + i * 16) = (u32x4){0, 0, 0, 0};
+    if ((cached >> key) & 1) continue;
+    lds_u32x4* at = reinterpret_cast<lds_u32x4*>(cur + KT * S::ROWB + i * 16);
+    u32x4 v = *at;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (BF16 && ((v[j] >> 16) & kExponent) == kExponent) v[j] &= 0xffffu;
+      if ((v[j] & kExponent) == kExponent) v[j] = BF16 ? v[j] & 0xffff0000u : 0u;
+    }
+    *at = v;
+  }
+}
+
+// One turn of a workgroup: tile `cur` has landed; the next one is copied into `other` while it is worked on.  `odd`: there was a key
+// that clean_tile would change.
 template <bool BF16, int DP, int MQ, int WK, typename Copy>
 __device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& x, lds_u8* __restrict cur, lds_u8* __restrict other, const uint32_t* valid,
-                                               int t0, int ctx, const uint16_t* s_up, float sc, bool active, Copy&& copy_next) {
+                                               int t0, int ctx, const uint16_t* s_up, float sc, bool active, bool careful, int last_word, bool& odd,
+                                               Copy&& copy_next) {
   // this wave's copies have landed, and behind the barrier the others'; all are done with the other buffer
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
   __syncthreads();
@@ -337,47 +402,12 @@ __device__ __forceinline__ void attention_turn(AttentionTile<BF16, DP, MQ, WK>& 
   uint64_t cached = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) cached |= (uint64_t)valid[w] << (w * (KT / 4));
+  odd |= cached != ~0ull;
+  if (careful) {
+    clean_tile<BF16, DP, MQ, WK>(cur, cached, last_word);
+    __syncthreads();
+  }
   if (active) x.step(cur, cur + KT * AttentionShape<BF16, DP, MQ, WK>::ROWB, cached, t0, ctx, s_up, sc);
-}
-
-// One query row of one head over the keys [from, to), key by key, by one wave: four elements of the head per lane.
-template <bool BF16>
-__device__ void row_by_keys(const AttentionJob& p, int q, int g, int row, int h, int ctx, int from, int to, f32x4& o, float& m, float& l) {
-  const int e = (opaque_tid() & 63) * 4;
-  auto four = [&](const void* at) {
-    f32x4 v = {0, 0, 0, 0};
-    if (e < p.head_dim) {
-      if constexpr (BF16) {
-        const uint64_t raw = *reinterpret_cast<const uint64_t*>(static_cast<const uint8_t*>(at) + e * 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = bf16_bits_to_f32((uint16_t)(raw >> (i * 16)));
-      } else {
-        v = *reinterpret_cast<const f32x4*>(static_cast<const uint8_t*>(at) + e * 4);
-      }
-    }
-    return v;
-  };
-  const f32x4 x = p.scale == 0 ? (f32x4){0, 0, 0, 0} : four(static_cast<const uint8_t*>(p.q) + q * p.q_seq + (int64_t)row * p.q_row + (int64_t)h * p.q_head);
-  o = (f32x4){0, 0, 0, 0}, m = kLowest, l = 0;
-  auto take = [&](int64_t at, const void* k, const void* v) {
-    const f32x4 y = four(static_cast<const uint8_t*>(k) + at);
-    const float score = wave_sum(x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3]) * (p.scale * kLog2e);
-    const float top = fmaxf(m, score), keep = __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(score - top);
-    o = o * keep + four(static_cast<const uint8_t*>(v) + at) * w;
-    l = l * keep + w;
-    m = top;
-  };
-  for (int key = from; key < min(to, ctx); ++key) {
-    const int b = key / p.block_size, x_ = p.block_table[(int64_t)q * p.max_blocks + b];
-    if (x_ >= 0 && x_ < p.n_blocks) take(x_ * p.block + (key - b * p.block_size) * p.slot + (int64_t)g * p.cache_head, p.k, p.v);
-  }
-  for (int n = 0;; ++n) {
-    if (n == kMaxStages) row = 0;
-    if (ctx + row >= from && ctx + row < to) take(q * p.new_seq + (int64_t)row * p.new_row + (int64_t)g * p.new_head, p.k_new, p.v_new);
-    if (row == 0) return;
-    const int up = p.node_parent[(int64_t)q * p.M + row - 1];
-    row = up >= 0 && up < row - 1 ? up + 1 : 0;
-  }
 }
 
 // A unit's tiles that a workgroup takes, in scalar registers.
@@ -643,7 +673,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   typedef TileCopy<BF16, DP, MQ, WK> Copy;
   constexpr int ESZ = S::ESZ, BM = S::BM;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  __shared__ uint32_t s_valid[2][4];
+  __shared__ uint32_t s_valid[2][4], s_again;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
   const int wq = wave / WK, wk = wave % WK;
   const int G = p.q_heads / p.kv_heads;
@@ -670,6 +700,8 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   typename Copy::Places f = copy.places(now, 0), f_next = {-1, 0};
   copy.copy(copy.source(now, 0, f), (lds_u8*)smem, s_valid[0]);
   int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
+  bool careful = false;        // the second pass over this share
+  if (tid == 0) s_again = 0;
   while (more) {
     Segment next = now;
     more = plan.following(next);
@@ -712,12 +744,13 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     if (now.n_tiles > 1) up = copy.source(now, 1, f);
     else up = first;
 
+    bool odd = last_word < S::CH - 1;
     const bool active = uniform(wq) * MQ * 16 < rows;   // (of a unit with few rows only the first waves have any: the others just copy)
     // ---- tiles.  The next one is copied into the other buffer while one is worked on; the two buffers are distinct objects to
     // the compiler (restrict), so that a read of one does not wait for the copies into the other ----
     auto tile = [&](lds_u8* cur, lds_u8* other, int t) {
       attention_turn<BF16, DP, MQ, WK>(
-          x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, active, [&](lds_u8* to) {
+          x, cur, other, s_valid[turn & 1], (now.tile0 + t) * KT, now.ctx, s_up, sc, active, careful, last_word, odd, [&](lds_u8* to) {
             if (up.k_cache) copy.copy(up, to, s_valid[(turn + 1) & 1]);
           });
       if (t + 2 < now.n_tiles) up = copy.source(now, t + 2, f);
@@ -769,39 +802,21 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
 
     // ---- out, or what has been summed so far ----
     const bool whole = now.n_seg == now.tiles;
-    if (!whole && now.tile0 == 0)   // the unit ends in the workgroup that takes its last tile
+    if (!whole && now.tile0 == 0)   // (the unit ends in the workgroup that takes its last tile)
       mine = {now.q, now.g, now.block, plan.last(), min(rows, BM)};
-    // A weight of zero does not take out a value that is not finite of a row that some of these rows do not see: sums that are not
-    // finite are found once more, from the keys that each row sees.  (Taking them out of every tile with rows of the tree ahead of
-    // the product, where there are any: 41 -> 46 us for 64 sequences of 100 tokens)
-    float zero = 0;
+    if (odd && !careful) {
+      float zero = 0;
 #pragma unroll
-    for (int mq = 0; mq < MQ; ++mq)
+      for (int mq = 0; mq < MQ; ++mq)
 #pragma unroll
-      for (int d = 0; d < DP / 16; ++d)
+        for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x.o[mq][d][i], 0.0f, zero);
-    if (wk == 0 && __any(!(zero == 0.0f))) {
-      const int wave_ = uniform(opaque_tid() >> 6), at = opaque_tid() & 63;
-      for (int i = 0; i < MQ * 16; ++i) {
-        const int m = (wave_ / WK) * MQ * 16 + i, row = (now.block * BM + m) / G, h = now.g * G + (now.block * BM + m) % G;
-        if (m >= rows) break;
-        f32x4 o;
-        float top, l;
-        row_by_keys<BF16>(p, now.q, now.g, row, h, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, o, top, l);
-        if (at * 4 >= p.head_dim) continue;
-        if (whole) {
-          o = o * (1.0f / l);
-          uint8_t* to = static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)row * p.out_row + (int64_t)h * p.out_head;
-          if constexpr (BF16) *reinterpret_cast<uint64_t*>(to + at * 8) = (uint64_t)f32_to_bf16_pair(o[2], o[3]) << 32 | f32_to_bf16_pair(o[0], o[1]);
-          else *reinterpret_cast<f32x4*>(to + at * 16) = o;
-        } else {
-          float* to = ws.part + ((int64_t)(me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + m) * (DP + 4);
-          *reinterpret_cast<f32x4*>(to + at * 4) = o;
-          if (at == 0) to[DP] = top, to[DP + 1] = l;
-        }
-      }
-    } else if (wk == 0) {
+          for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x.o[mq][d][i], 0.0f, zero);
+      if (wk == 0 && __any(!(zero == 0.0f)) && lane == 0) s_again = 1;
+    }
+    if (careful && wk == 0 && (now.tile0 + now.n_tiles) * KT > now.ctx)
+      add_left_out(x, now.k_rows, copy.to_v_rows, p.new_row, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, s_up, last_word);
+    if (wk == 0) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
         const int m = (wq * MQ + mq) * 16 + l16;
@@ -831,6 +846,15 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
     now = next;
     f = f_next;
     ++n_units;
+    if (!more && !careful) {
+      __syncthreads();
+      if (s_again) {
+        careful = true;
+        more = plan.first(now);
+        f = copy.places(now, 0);
+        copy.copy(copy.source(now, 0, f), (lds_u8*)(smem + (turn & 1) * (S::LDS / 2)), s_valid[turn & 1]);
+      }
+    }
   }
   if (tid == 0) ws.owner[me] = mine;
 }
