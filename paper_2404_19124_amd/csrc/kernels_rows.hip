@@ -12,7 +12,10 @@
 namespace specdraft {
 
 constexpr int row_chunks(bool out) { return out ? 1 : 2; }   // chunks of 8 tokens that a thread has in flight
-constexpr int kWideRows = 512;   // rows of which two fit a CU: 1024 threads each (34 rows of 32000: 12.7 us, with 512: 15.4 us)
+// Up to so many rows have 1024 threads each, in more 512.  A verification of rows of 32000 with 1024 and with 512: 34 float32 rows 13.5
+// and 16.4 us, 256 rows 19.3 and 22.3; from 280 to 500, where two rows share a CU (bfloat16) or take turns (float32: 120 KiB of LDS
+// each), 25.9 to 30.2 and 26.4 to 29.3, alike; 650 bfloat16 rows 32.4 and 25.4, float32 38.2 and 40.5.
+constexpr int kWideRows = 512;
 
 // eight neighbours; rows of an odd length start anywhere, so their words are not aligned to 16 bytes (the compiler's memcpy is one
 // 16-byte load all the same)

@@ -326,6 +326,21 @@ def test_many_rows(dtype, V):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,M", [(512, 0), (513, 0), (128, 3), (19, 26), (1, 511), (1, 512)])
+def test_where_rows_get_fewer_threads(b, M, dtype):
+    """512 rows of a call have 1024 threads each, 513 have 512: the first maxima of both, none on a tie's later place."""
+    R, V = M + 1, 8200
+    r = Rows(b, M, V, dtype, seed=b, values="ties", n_nodes=[M] * b)
+    want = every_row_on_the_device(r)
+    got = [torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((b, R), (b,), (b,), (b, 1), (b,), (b, 1))]
+    none = torch.zeros((b, 1, 0), dtype=torch.int32, device="cuda")
+    B.spec_verify_tree(r.logits, none, none, dev(r.n_nodes), *got, penalties=r.dev_pen())
+    best = want.max(-1, keepdim=True).values
+    assert torch.equal(got[0], (want == best).int().argmax(-1).int())
+    assert torch.equal(got[3][:, 0], got[0][:, 0]) and (got[1] == 0).all() and (got[4] == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_captured_replayed_and_on_another_stream(dtype):
     """The captured call reads what its arguments hold at the replay; a call on another stream while it runs does not disturb it."""
     r, cand, node = agreeing(3, 8, 3, 4099, dtype, seed=31)
