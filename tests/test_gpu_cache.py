@@ -185,3 +185,34 @@ def test_where_one_kernel_becomes_two(b, cap):
     add[b // 2] = 9000 if b == 1 else -10 ** 6
     s.step(add, cap=cap, in_place=True)
     s.step([1] * b, cap=cap, path=[[4, 2]] * b, seq_rows=5)
+
+
+@pytest.mark.parametrize("b", [1025, 3000, 65535])
+def test_large_batches(b):
+    """Growth, ends and shortage in batches of which a workgroup takes several sequences."""
+    rng = np.random.default_rng(b)
+    s = Server(rng, b, 4, [0] * b, 3 * b, 6)
+    for share in (0.9, 0.5, 0.2):
+        add = np.where(rng.random(b) < share, rng.integers(0, 9, b), np.where(rng.random(b) < 0.5, -10 ** 6, -rng.integers(0, 5, b)))
+        s.step(add.tolist(), cap=max(5000, 6 * b), path=rng.integers(0, 4, (b, 3)).tolist(), seq_rows=4)
+
+
+def test_the_largest_batch_takes_a_time_like_its_size():
+    """65535 sequences against 2047: a hundred times at most (32 times the sequences; all of them summed up per sequence is a thousand
+    times the work, and took two thousand times as long)."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    took = []
+    for b in (2047, 65535):
+        add, z = torch.full((b,), 3, **i32), lambda *s: torch.zeros(s, **i32)
+        args = (z(b), add, z(b), z(b), z(b, 2), torch.arange(b, **i32), torch.tensor([0, b], **i32), z(2), 16, z(b + 1), z(4 * b))
+        best = np.inf
+        for _ in range(5):
+            t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            t[0].record()
+            B.spec_cache_extend(*args)
+            t[1].record()
+            torch.cuda.synchronize()
+            best = min(best, t[0].elapsed_time(t[1]))
+        assert args[3].eq(3).all()
+        took.append(best)
+    assert took[1] < 100 * took[0], took
