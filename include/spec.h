@@ -321,7 +321,8 @@ typedef struct {
  *   node_parent dev [batch, M] int32 as spec_tree_metadata writes it (a parent comes before its node; -1: child of
  *               row 0); may be NULL if M = 0.  A chain of parents is followed over SPEC_MAX_STAGES nodes, the row's own among them
  *   n_nodes     dev [batch] int32 in [-1, M]; NULL: M everywhere
- * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.
+ * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.  No two rows of out share
+ * memory (refused by the strides: in the order of their sizes, each has to leave behind what those before it span).
  * A cached token whose block is outside [0, n_blocks) takes no part.  Cache slots at and past ctx_len, and rows of k_new and v_new
  * behind the last node, may hold anything.
  * Infinities and NaN among the keys and values of a row reach the rows that see it and no others.  (They cost time: the workgroups
@@ -371,7 +372,8 @@ spec_status_t spec_cache_extend(const int32_t* ctx_len, const int32_t* add, int3
  *     cache[l][slot[t]] = new[l][src_row ? src_row[t] : t]        for t < count, slot[t] in [0, n_blocks * block_size)
  * Entries with another slot, or a source row outside [0, rows), are skipped.  The slots of one call are distinct.
  *   k_new, v_new  rows of kv_heads; seq_stride is the distance of two layers
- *   cache         written; cache_layer_stride is the distance of two of its layers, in elements
+ *   cache         written; cache_layer_stride is the distance of two of its layers, in elements.  No two rows of k share memory, nor
+ *                 of v (refused as for spec_tree_attention's out)
  *   head_dim      as for spec_tree_attention;  slot, src_row dev int32 [count]; src_row may be NULL */
 spec_status_t spec_cache_store(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_cache_t* cache,
                                int64_t cache_layer_stride, int32_t layers, int32_t rows, int32_t kv_heads, int32_t head_dim,

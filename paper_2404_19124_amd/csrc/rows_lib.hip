@@ -1,4 +1,8 @@
 // C ABI of the operators on the rows of a token tree (declared in include/spec.h): argument checks and launches.
+#include <algorithm>
+#include <initializer_list>
+#include <utility>
+
 #include "rows_internal.h"
 #include "spec_internal.h"
 #include "status.h"
@@ -13,6 +17,22 @@ static bool rows_aligned(const void* at, int64_t a, int64_t b, int64_t c, int es
   return !(((uint64_t)reinterpret_cast<uintptr_t>(at) | (uint64_t)(a * esz) | (uint64_t)(b * esz) | (uint64_t)(c * esz)) & 15);
 }
 static bool rows_aligned(const spec_rows_t& r, int esz) { return rows_aligned(r.at, r.seq_stride, r.row_stride, r.head_stride, esz); }
+
+// Whether no two rows of `row` elements share memory, counted along dimensions of n entries and these strides: in the order of the
+// strides' sizes, each dimension's step leaves the extent of those before it behind (so do slices and permutations of a tensor)
+static bool rows_apart(std::initializer_list<std::pair<int64_t, int64_t>> dims, int64_t row) {
+  std::pair<__int128, int64_t> d[4];
+  int n = 0;
+  for (const auto& x : dims)
+    if (x.first > 1) d[n++] = {x.second < 0 ? -(__int128)x.second : (__int128)x.second, x.first};
+  std::sort(d, d + n);
+  __int128 extent = row;
+  for (int i = 0; i < n; ++i) {
+    if (d[i].first < extent) return false;
+    extent += d[i].first * (d[i].second - 1);
+  }
+  return true;
+}
 
 static spec_status_t check_heads(int32_t dtype, int32_t kv_heads, int32_t head_dim) {
   if (!known_dtype(dtype)) return fail(SPEC_EDTYPE, "dtype = %d is neither SPEC_F32 nor SPEC_BF16", dtype);
@@ -75,6 +95,8 @@ extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_ro
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SPEC_EINVAL, "workspace of %lld bytes, needed are %lld", (long long)(workspace ? workspace_bytes : 0), (long long)need);
   if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(SPEC_EINVAL, "workspace must be 16-byte aligned");
+  if (!rows_apart({{batch, out->seq_stride}, {M + 1, out->row_stride}, {q_heads, out->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of out overlap");
   AttentionJob j;
   j.q = q->at, j.k_new = k_new->at, j.v_new = v_new->at, j.k = cache->k, j.v = cache->v, j.out = const_cast<void*>(out->at);
   j.q_seq = q->seq_stride * esz, j.q_row = q->row_stride * esz, j.q_head = q->head_stride * esz;
@@ -139,6 +161,8 @@ extern "C" spec_status_t spec_cache_store(const spec_rows_t* k_new, const spec_r
   if (!rows_aligned(*k_new, esz) || !rows_aligned(*v_new, esz) || ((uint64_t)(cache_layer_stride * esz) & 15))
     return fail(SPEC_EINVAL, "rows of k_new, v_new and the cache must start on multiples of 16 bytes");
   if ((int64_t)kv_heads * head_dim > 1 << 24) return fail(SPEC_ESHAPE, "kv_heads * head_dim is too large");
+  if (!rows_apart({{layers, cache_layer_stride}, {cache->n_blocks, cache->block_stride}, {cache->block_size, cache->slot_stride}, {kv_heads, cache->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of the cache overlap");
   StoreJob j;
   j.k_new = static_cast<const uint8_t*>(k_new->at), j.v_new = static_cast<const uint8_t*>(v_new->at);
   j.k = static_cast<uint8_t*>(const_cast<void*>(cache->k)), j.v = static_cast<uint8_t*>(const_cast<void*>(cache->v));

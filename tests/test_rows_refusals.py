@@ -216,3 +216,33 @@ def test_binding_penalties(monkeypatch):
                       (dict(logits=z((2, 3, 70), dtype=torch.half)), "float32 or bfloat16")):
         with pytest.raises(ValueError, match=words):
             B.spec_verify_tree(**dict(v, **kw))
+
+
+# ---- what is written must not hold an element twice ------------------------------------------------------------------
+
+APART = dict(batch=2, M=4, q_heads=4, kv_heads=2, head_dim=8, workspace=P)
+
+
+@pytest.mark.parametrize("out", [rows(seq=128, row=64, head=8), rows(seq=512, row=24, head=8), rows(seq=512, row=64, head=0), rows(seq=0, row=64, head=8),
+                                 rows(seq=-64, row=64, head=8), rows(seq=32, row=-8, head=80)])
+def test_attention_outputs_that_overlap(out):
+    """Strides that are not zero and yet lead to the same memory."""
+    assert attention(out=out, **APART) == B.SPEC_EINVAL and "overlap" in B.spec_last_error(), B.spec_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(layer=0), dict(layer=512), dict(cache=cache(block_stride=128)), dict(cache=cache(slot_stride=8)),
+                                dict(cache=cache(slot_stride=-8)), dict(cache=cache(head_stride=0)), dict(cache=cache(block_stride=16, slot_stride=24))])
+def test_stores_into_a_cache_that_overlaps(kw):
+    assert store(**kw) == B.SPEC_EINVAL and "overlap" in B.spec_last_error(), B.spec_last_error()
+
+
+def test_binding_refuses_outputs_that_overlap(monkeypatch):
+    monkeypatch.setattr(B, "_CHECK_DEVICE", False)
+    t = tensors()
+    t["workspace"] = torch.zeros(B.spec_tree_attention_workspace(2, 5, 4, 2, 16, torch.float32), dtype=torch.uint8)
+    with pytest.raises(B.SpecError, match="rows of out overlap"):
+        B.spec_tree_attention(**dict(t, out=torch.zeros(2000).as_strided((2, 5, 4, 16), (320, 32, 16, 1)), stream=STREAM))
+    z = torch.zeros
+    with pytest.raises(B.SpecError, match="rows of the cache overlap"):
+        k = z(2000).as_strided((3, 8, 2, 16), (128, 32, 16, 1))
+        B.spec_cache_store(z((5, 2, 16)), z((5, 2, 16)), z((4,), **I32), k, k, stream=STREAM)
