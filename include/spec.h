@@ -408,7 +408,8 @@ typedef struct {
  *   logits, out [batch, R, vocab] logits_dtype; out may be logits.  Rows behind the last node are left as they were
  *   node_tok, node_parent [batch, M], n_nodes [batch]: as for spec_tree_attention; node_tok, node_parent may be NULL
  *   (no path counts), n_nodes NULL: M everywhere
- *   pen  host */
+ *   pen  host
+ * Limits, of spec_verify_tree too: M <= 4096, batch * R <= 2^23 - 8, vocab <= 2^30. */
 spec_status_t spec_penalize(const void* logits, int32_t logits_dtype, int32_t batch, int32_t M, int32_t vocab,
                             const spec_penalties_t* pen, const int32_t* node_tok, const int32_t* node_parent,
                             const int32_t* n_nodes, void* out, void* hip_stream);

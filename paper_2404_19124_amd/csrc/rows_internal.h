@@ -10,6 +10,8 @@ namespace specdraft {
 
 constexpr int64_t kMaxSlots = 1 << 30;   // tokens of a cache, of a block table's row, of a slot map
 
+constexpr int kMaxLogitsRows = (1 << 23) - 8;   // rows of one call on logits
+
 // ---- attention of the rows over a paged cache and their own ancestors ----------------
 struct AttentionJob {
   const void *q, *k_new, *v_new, *k, *v;

@@ -182,7 +182,8 @@ static spec_status_t check_logits(const void* logits, int32_t dtype, int32_t bat
   if (!known_dtype(dtype)) return fail(SPEC_EDTYPE, "logits_dtype = %d is neither SPEC_F32 nor SPEC_BF16", dtype);
   if (batch < 1 || M < 0 || vocab < 1) return fail(SPEC_EINVAL, "batch and vocab must be >= 1, M >= 0");
   if (M > kMaxTreeItems) return fail(SPEC_ESHAPE, "M = %d exceeds %d", M, kMaxTreeItems);
-  if ((int64_t)batch * (M + 1) > 0x7fffffffLL) return fail(SPEC_ESHAPE, "batch * (M + 1) is too large");
+  // (a launch has fewer than 2^32 threads, and a row up to 512 of them in so many rows)
+  if ((int64_t)batch * (M + 1) > kMaxLogitsRows) return fail(SPEC_ESHAPE, "batch * (M + 1) = %lld exceeds %d", (long long)batch * (M + 1), kMaxLogitsRows);
   if (vocab > 1 << 30) return fail(SPEC_ESHAPE, "vocab exceeds 2^30");
   if (!node_tok != !node_parent) return fail(SPEC_EINVAL, "node_tok and node_parent go together");
   if (pen) {

@@ -130,6 +130,13 @@ def test_verify(kw, status):
     assert verify(**kw) == status, B.spec_last_error()
 
 
+@pytest.mark.parametrize("call", [penalize, verify])
+def test_rows_past_a_launch(call):
+    """More rows than workgroups of 512 threads fit a launch of 2^32 threads."""
+    for batch, M in (((1 << 23) - 7, 0), (1 << 20, 8), (1 << 15, 256), (2048, 4095)):
+        assert call(batch=batch, M=M) == B.SPEC_ESHAPE, (batch, M, B.spec_last_error())
+
+
 # ---- the binding's own checks -------------------------------------------------------------------------------------
 
 I32 = dict(dtype=torch.int32)
