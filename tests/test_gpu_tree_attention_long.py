@@ -1,0 +1,151 @@
+"""spec_tree_attention where a workgroup's share of a unit is many tiles long, in trees of up to 4096 nodes, and through strides that a
+tensor cannot have.  Against 64 bits on the device: the oracle's loops would take hours."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rows_oracle as RO
+from paper_2404_19124_amd import binding as B
+from tests.rows_common import U16, attention_bound, dev, exact_float
+from tests.test_gpu_tree_attention import Case
+
+pytestmark = pytest.mark.gpu
+TILE = 64
+
+
+def on_device(c):
+    """What RO.attention returns, from products of matrices in float64; rows that do not exist hold NaN."""
+    q, kn, vn, k, v = (t.double() for t in (c.q, c.k_new, c.v_new, c.k, c.v))
+    out, weighted = torch.full_like(q, float("nan")), torch.full_like(q, float("nan"))
+    products, most, G = 0.0, 0, c.H // c.KH
+    for s in range(c.b):
+        n, live = int(c.ctx[s]), int(c.n_nodes[s]) + 1
+        if live == 0:
+            continue
+        t = np.arange(n)
+        block = c.table[s][t // c.page].astype(np.int64)
+        there = (block >= 0) & (block < c.k.shape[0])
+        at = torch.as_tensor(block[there] * c.page + t[there] % c.page, device="cuda")
+        sees = torch.zeros((live, live), dtype=torch.bool)
+        for r in range(live):
+            sees[r, [0] + [x + 1 for x in RO.path_of(c.parent[s] if c.M else [], r)]] = True
+        sees = sees.cuda().repeat_interleave(G, 0)
+        for g in range(c.KH):
+            keys = torch.cat([k.view(-1, c.KH, c.D)[at, g], kn[s, :live, g]])
+            values = torch.cat([v.view(-1, c.KH, c.D)[at, g], vn[s, :live, g]])
+            rows = q[s, :live, g * G:(g + 1) * G].reshape(live * G, c.D)
+            z = rows @ keys.T.contiguous() * c.scale
+            z[:, len(at):][~sees] = float("-inf")
+            p = torch.softmax(z, 1)
+            out[s, :live, g * G:(g + 1) * G] = (p @ values).view(live, G, c.D)
+            weighted[s, :live, g * G:(g + 1) * G] = (p @ values.abs()).view(live, G, c.D)
+            # (of all rows of the tree: an upper bound)
+            products = max(products, float((rows.abs() @ keys.abs().T.contiguous()).max()) * abs(c.scale))
+            most = max(most, len(at) + live)
+    return out.cpu().numpy(), weighted.cpu().numpy(), products, most
+
+
+def check(c, got, before=7.0):
+    out, weighted, products, keys = on_device(c)
+    bf16 = c.dtype == torch.bfloat16
+    # (a weight's rounding is in its sum, too: U16 of the result)
+    bound = attention_bound(out, weighted, products, keys, c.D, bf16) + (U16 * np.abs(out) if bf16 else 0)
+    g = exact_float(got)
+    for s in range(c.b):
+        live = int(c.n_nodes[s]) + 1
+        off = np.abs(g[s, :live] - out[s, :live])
+        assert bool((off <= bound[s, :live]).all()), (s, float((off / bound[s, :live]).max()))
+        assert bool((g[s, live:] == before).all()), s
+
+
+# heads, key/value heads, head, nodes, sequences, tokens, type, workgroups of the launch, query rows of a unit, tiles of a share
+LONG = {
+    "keys_over_four_waves": (2, 2, 64, 3, 64, 290, "bf16", 512, 16, 70),
+    "two_blocks_of_rows": (12, 1, 128, 12, 64, 290, "bf16", 512, 128, 70),
+    "keys_over_two_waves": (3, 3, 128, 20, 44, 290, "bf16", 512, 32, 70),
+    "more_than_128_tiles": (2, 2, 128, 40, 124, 300, "bf16", 512, 64, 140),
+    "one_unit_over_many": (2, 1, 128, 7, 3, 16000, "bf16", 512, 16, 90),
+    "wide_heads": (4, 2, 256, 5, 32, 290, "bf16", 256, 16, 70),
+    "float32": (2, 2, 64, 3, 64, 290, "f32", 512, 16, 70),
+    "float32_of_80": (4, 1, 80, 9, 64, 290, "f32", 256, 64, 70),
+    "float32_more_than_128_tiles": (2, 2, 128, 8, 62, 300, "f32", 256, 16, 140),
+    "float32_wide_heads": (2, 1, 160, 3, 128, 290, "f32", 512, 16, 70),
+}
+
+
+@pytest.mark.parametrize("name", LONG)
+def test_long_shares(name):
+    """Tables that repeat a small pool of blocks.  A few blocks of each are loud, with all weight but a few hundredths, and values of
+    their own: any of them that is left out, read twice or taken for another moves a result by its hundredths of the weight, many times
+    what the bound allows.  They lie at the ends of the first, the 64th and the 128th tile, and anywhere; one behind them is out
+    of range."""
+    H, KH, D, M, b, tiles, dtype, groups, rows, share = LONG[name]
+    rng = np.random.default_rng(len(name))
+    c = Case(H, KH, D, 16, M, [1] * b, dtype, seed=len(name))
+    gen = torch.Generator().manual_seed(len(name))
+    c.ctx = np.array([tiles * TILE - int(rng.integers(0, 5 * TILE)) for _ in range(b)], np.int32)
+    cost = 2 if dtype == "bf16" else 1
+    units = sum((-(-(n + m + 1) // TILE) + cost) * -(-(m + 1) * (H // KH) // rows) * KH for n, m in zip(c.ctx.tolist(), c.n_nodes.tolist()))
+    assert units >= share * groups
+    c.k, c.v = (torch.randn((64, 16, KH, D), generator=gen).to(c.dtype).cuda() for _ in range(2))
+    c.q[..., 0] = 4
+    loud = torch.randn((8, 1, KH, D), generator=gen).to(c.dtype).cuda()
+    c.k[:8, :, :, 0] = (7 + np.log(tiles / 290)) * D ** 0.5 / 4
+    c.v[:8] = loud + c.v[:8] / 16
+    width = -(-int(c.ctx.max()) // 16)
+    c.table = rng.integers(8, 64, (b, width)).astype(np.int32)
+    for s in range(b):
+        spots = rng.choice(width - 8, 24, replace=False).tolist() + [0, 3, 4, 252, 255, 256, 259, 260, 511, 512, int(c.ctx[s] - 1) // 16]
+        c.table[s, [x for x in spots if x < width]] = rng.integers(0, 8, len([x for x in spots if x < width]))
+        c.table[s, 300 + int(rng.integers(100))] = (-1, 64, 2 ** 31 - 1)[s % 3]
+    check(c, c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,KH,D,M,ctx", [(2, 1, 64, 4096, [70, 0]), (1, 1, 128, 4095, [130]), (4, 1, 80, 1000, [40, 300, 5]), (1, 1, 256, 2000, [65]),
+                                          (2, 2, 192, 600, [33, 1])])
+def test_trees_of_many_nodes(H, KH, D, M, ctx, dtype):
+    """Up to 4096 nodes: the parents of two segments at a time lie in the memory behind the tiles."""
+    c = Case(H, KH, D, 16, M, ctx, dtype, seed=81)
+    check(c, c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 80, 160])
+def test_a_scale_of_zero_weighs_all_keys_alike(D, dtype):
+    c = Case(6, 2, D, 16, 9, [100, 0, 33], dtype, seed=82)
+    c.scale = 0.0
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 80, 160])
+def test_strides_that_go_backwards(D, dtype):
+    """Sequences, rows, heads, blocks and slots in falling order, through the C entry (a tensor has no negative strides)."""
+    H, KH = 6, 2
+    c = Case(H, KH, D, 16, 12, [100, 31, 0, 64], dtype, seed=83)
+    esz = c.q.element_size()
+
+    def rows(t, flip):
+        """The same rows from a copy whose dimensions in `flip` are turned over."""
+        x = t.flip(flip).contiguous()
+        keep.append(x)
+        stride = [-x.stride(i) if i in flip else x.stride(i) for i in range(t.dim() - 1)]
+        return x, x.data_ptr() + esz * sum(x.stride(i) * (x.shape[i] - 1) for i in flip), stride
+
+    keep = []
+    for flips, cache_flip in (((0, 1, 2), (0, 1, 2)), ((1,), (0,)), ((0,), (1,)), ((2,), (2,))):
+        out = torch.full(c.q.shape, 7.0, dtype=c.dtype, device="cuda")
+        x, at, stride = rows(out, flips)
+        parts = [B.spec_rows_t(p, *st) for _, p, st in (rows(t, flips) for t in (c.q, c.k_new, c.v_new))]
+        (_, k, ck), (_, v, _) = rows(c.k, cache_flip), rows(c.v, cache_flip)
+        cache = B.spec_cache_t(k, v, *ck, c.k.shape[0], 16)
+        space, ints = c.workspace(), [dev(t) for t in (c.table, c.ctx, c.parent, c.n_nodes)]
+        status = B.lib().spec_tree_attention(*[C.byref(p) for p in parts], C.byref(cache), *[t.data_ptr() for t in ints], C.byref(B.spec_rows_t(at, *stride)),
+                                             c.b, c.M, H, KH, D, B.SPEC_BF16 if dtype == "bf16" else B.SPEC_F32, c.table.shape[1], c.scale,
+                                             space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert status == B.SPEC_OK, B.spec_last_error()
+        c.check(x.flip(flips))
