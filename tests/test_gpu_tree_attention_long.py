@@ -66,7 +66,7 @@ LONG = {
     "two_blocks_of_rows": (12, 1, 128, 12, 64, 290, "bf16", 512, 128, 70),
     "keys_over_two_waves": (3, 3, 128, 20, 44, 290, "bf16", 512, 32, 70),
     "more_than_128_tiles": (2, 2, 128, 40, 124, 300, "bf16", 512, 64, 140),
-    "one_unit_over_many": (2, 1, 128, 7, 3, 16000, "bf16", 512, 16, 90),
+    "one_unit_over_many": (2, 1, 128, 7, 30, 1600, "bf16", 512, 16, 90),
     "wide_heads": (4, 2, 256, 5, 32, 290, "bf16", 256, 16, 70),
     "float32": (2, 2, 64, 3, 64, 290, "f32", 512, 16, 70),
     "float32_of_80": (4, 1, 80, 9, 64, 290, "f32", 256, 64, 70),
