@@ -83,6 +83,13 @@ def test_penalize(b, M, V, dtype):
     Rows(b, M, V, dtype, seed=V).check_penalized()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,M,V", [(1, 4096, 40), (2, 2500, 9)])
+def test_penalize_trees_of_many_nodes(b, M, V, dtype):
+    """Up to 4096 nodes, whose parents and tokens lie where the touched chunks are listed afterwards."""
+    Rows(b, M, V, dtype, seed=M).check_penalized()
+
+
 @pytest.mark.parametrize("keep", [(), ("counts",), ("seen",), ("seen", "repetition"), ("counts", "repetition", "presence"), ("bias",), ("allowed",),
                                   ("frequency", "presence", "repetition")])
 @pytest.mark.parametrize("path", [False, True])
