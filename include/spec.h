@@ -322,7 +322,8 @@ typedef struct {
  *               row 0); may be NULL if M = 0.  A chain of parents is followed over SPEC_MAX_STAGES nodes, the row's own among them
  *   n_nodes     dev [batch] int32 in [-1, M]; NULL: M everywhere
  * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.  No two rows of out share
- * memory (refused by the strides: in the order of their sizes, each has to leave behind what those before it span).
+ * memory (refused by the strides: in the order of their sizes, each has to leave behind what those before it span); out may be q, and
+ * overlaps nothing else.
  * A cached token whose block is outside [0, n_blocks) takes no part.  Cache slots at and past ctx_len, and rows of k_new and v_new
  * behind the last node, may hold anything.
  * Infinities and NaN among the keys and values of a row reach the rows that see it and no others.  (They cost time: the workgroups

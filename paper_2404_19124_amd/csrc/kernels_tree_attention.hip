@@ -701,6 +701,9 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
   copy.copy(copy.source(now, 0, f), (lds_u8*)smem, s_valid[0]);
   int turn = 0, n_units = 0;   // tiles and segments so far: which buffers are in use
   bool careful = false;        // the second pass over this share
+  // The first segment whose sums in this wave are not finite, and the first of this pass: the wave has written its outputs before that
+  // one in the first pass, and writes the others in the second (out may be q: what is read again has not been written).
+  int first_odd = 1 << 30, unit0 = 0;
   if (tid == 0) s_again = 0;
   while (more) {
     Segment next = now;
@@ -812,11 +815,14 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
         for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x.o[mq][d][i], 0.0f, zero);
-      if (wk == 0 && __any(!(zero == 0.0f)) && lane == 0) s_again = 1;
+      if (wk == 0 && __any(!(zero == 0.0f))) {
+        if (lane == 0) s_again = 1;
+        first_odd = min(first_odd, n_units);
+      }
     }
     if (careful && wk == 0 && (now.tile0 + now.n_tiles) * KT > now.ctx)
       add_left_out(x, now.k_rows, copy.to_v_rows, p.new_row, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, s_up, last_word);
-    if (wk == 0) {
+    if (wk == 0 && (careful ? n_units - unit0 >= first_odd : n_units < first_odd)) {
 #pragma unroll
       for (int mq = 0; mq < MQ; ++mq) {
         const int m = (wq * MQ + mq) * 16 + l16;
@@ -850,6 +856,7 @@ __global__ __launch_bounds__(256, tile_bytes(KT * DP * (BF16 ? 2 : 4)) <= 65536 
       __syncthreads();
       if (s_again) {
         careful = true;
+        unit0 = n_units;
         more = plan.first(now);
         f = copy.places(now, 0);
         copy.copy(copy.source(now, 0, f), (lds_u8*)(smem + (turn & 1) * (S::LDS / 2)), s_valid[turn & 1]);

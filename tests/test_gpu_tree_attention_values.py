@@ -127,3 +127,24 @@ def test_a_key_of_minus_infinity_has_no_weight(H, KH, D, M, ctx, dtype):
         left.append(len(keep))
     args.update(k_cache=k2, v_cache=v2, table=table, ctx=np.array(left, np.int32))
     check_attention(got, args, c.n_nodes, torch.full(got.shape, 7.0, dtype=c.dtype))
+
+
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,KH,D,M,ctx", [(2, 2, 64, 3, [40, 0, 9]), (8, 2, 128, 30, [200, 17]), (16, 1, 128, 20, [70]), (4, 4, 64, 12, [(37 * i) % 150 for i in range(150)]),
+                                          (12, 2, 256, 9, [700, 3]), (4, 1, 96, 40, [64, 130, 5]), (2, 1, 160, 12, [90, 2000]), (6, 3, 128, 6, [3000, 1])])
+def test_outputs_in_the_place_of_the_queries(H, KH, D, M, ctx, dtype, odd):
+    """The same bits as into memory of its own; with infinities, too, which some shares are gone through twice for."""
+    c = Case(H, KH, D, 16, M, ctx, dtype, seed=76)
+    if odd:
+        for q in range(0, c.b, 3):
+            c.v_new[q, min(2, M), KH - 1, 3] = float("inf")
+            if ctx[q]:
+                c.v[int(c.table[q, 0]), 0, 0, 1] = float("-inf")
+    want = c.run()
+    q = c.q.clone()
+    got = c.run(out=q, q=q)
+    for s in range(c.b):
+        live = int(c.n_nodes[s]) + 1
+        assert torch.equal(got[s, :live].nan_to_num(nan=1e30), want[s, :live].nan_to_num(nan=1e30)), s
+        assert torch.equal(got[s, live:], c.q[s, live:])
