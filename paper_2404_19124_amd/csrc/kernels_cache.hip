@@ -98,6 +98,7 @@ __global__ __launch_bounds__(256) void extend_fill_kernel(ExtendJob p, int stret
     return;
   }
   const int first_q = blockIdx.x * stretch, last_q = min(first_q + stretch, p.batch);
+  int a = p.added[first_q], now = p.new_len[first_q], first = p.row_start[first_q];   // (requested ahead)
   uint64_t sum[4] = {0, 0, 0, 0};   // blocks taken and given back: before the next sequence, by all
   for (int i = tid; i < p.batch; i += 256) {
     const int d = p.added[i], now = p.new_len[i];
@@ -118,19 +119,12 @@ __global__ __launch_bounds__(256) void extend_fill_kernel(ExtendJob p, int stret
   // (the ring before this call)
   const uint64_t head = ((uint64_t)p.ring_state_new[0] + n - sum[2] % n) % n;
   const uint64_t count = (uint64_t)p.ring_state_new[1] + sum[2] - sum[3];
-  for (int q = first_q; q < last_q; ++q) {
-    const int a = p.added[q];
-    if (a == 0) continue;
-    const int now = p.new_len[q], old = now - a;
+  for (int q = first_q;;) {
+    const int old = now - a;
     const int have = blocks_of(old, p.block_size), want = blocks_of(now, p.block_size);
     int32_t* row = p.block_table + (int64_t)q * p.max_blocks;
-    if (a < 0) {
-      for (int i = want + at; i < have; i += step) p.ring[(head + count + sum[1] + (uint64_t)(i - want)) % n] = row[i];
-      sum[1] += (uint64_t)(have - want);
-      continue;
-    }
+    for (int i = want + at; i < have; i += step) p.ring[(head + count + sum[1] + (uint64_t)(i - want)) % n] = row[i];
     for (int i = have + at; i < want; i += step) row[i] = p.ring[(head + sum[0] + (uint64_t)(i - have)) % n];
-    const int first = p.row_start[q];
     for (int j = at; j < a; j += step) {
       const int t = old + j, b = t / p.block_size;
       // (a new block's entry may be under way to the table)
@@ -142,7 +136,10 @@ __global__ __launch_bounds__(256) void extend_fill_kernel(ExtendJob p, int stret
         p.src_row[first + j] = r >= 0 && r < p.seq_rows ? q * p.seq_rows + r : -1;
       }
     }
-    sum[0] += (uint64_t)(want - have);
+    sum[0] += (uint64_t)max(want - have, 0);
+    sum[1] += (uint64_t)max(have - want, 0);
+    if (++q == last_q) return;
+    a = p.added[q], now = p.new_len[q], first = p.row_start[q];
   }
 }
 
