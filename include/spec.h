@@ -322,12 +322,14 @@ typedef struct {
  *               row 0); may be NULL if M = 0.  A chain of parents is followed over SPEC_MAX_STAGES nodes, the row's own among them
  *   n_nodes     dev [batch] int32 in [-1, M]; NULL: M everywhere
  * Rows behind the last node, and all rows of a sequence that takes no part, are neither read nor written.  No two rows of out share
- * memory (refused by the strides: in the order of their sizes, each has to leave behind what those before it span); out may be q, and
- * overlaps nothing else.
+ * memory (refused by the strides: in the order of their sizes, each has to leave behind what those before it span); out may be q,
+ * row for row, and overlaps nothing else.
  * A cached token whose block is outside [0, n_blocks) takes no part.  Cache slots at and past ctx_len, and rows of k_new and v_new
  * behind the last node, may hold anything.
  * Infinities and NaN among the keys and values of a row reach the rows that see it and no others.  (They cost time: the workgroups
  * whose shares of the keys hold one beside rows of a tree, absent blocks or heads that are not 64, 128 or 256 wide do them twice.)
+ * The same call gives the same bits.  The order in which a row's keys are summed depends on the lengths of the whole batch, so a
+ * sequence in another batch may differ in its results' last bits.
  *   workspace   dev, 16-byte aligned, at least spec_tree_attention_workspace() bytes, contents of no meaning before
  *               and after; calls that may overlap in time, replays of graphs among them, need one each
  * Limits: M <= 4096, batch and q_heads <= 65535, max_blocks * block_size <= 2^30. */

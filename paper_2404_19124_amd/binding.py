@@ -604,7 +604,7 @@ def spec_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tenso
     q, out [batch, R, q_heads, head_dim]; k_new, v_new [batch, R, kv_heads, head_dim]; k_cache, v_cache [n_blocks, block_size,
     kv_heads, head_dim]: any strides but along head_dim, rows on 16 bytes, the same strides in k_* and v_*.  node_parent [batch, M]
     (None: M = 0), n_nodes [batch] (None: M each).  workspace: contiguous uint8, spec_tree_attention_workspace() bytes, not
-    shared by calls that may overlap in time.  scale: head_dim ** -0.5 by default."""
+    shared by calls that may overlap in time.  scale: head_dim ** -0.5 by default.  out may be q."""
     if _CHECK_DEVICE and _done((_fast or _native()).tree_attention(
             q, k_new, v_new, k_cache, v_cache, block_table, ctx_len, node_parent, n_nodes, out, workspace, scale, stream)):
         return

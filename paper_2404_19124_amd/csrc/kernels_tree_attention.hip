@@ -7,10 +7,10 @@
 // query row, a bound m of the scores so far, the sum l of the softmax's weights exp(score - m) and the weighted sum o of the
 // values (with a larger bound m', l and o are multiplied by exp(m - m')).
 //
-// Bound by reading the keys and values where a key/value head has few query rows, by the vector and matrix units where it has many,
-// by latency in small calls: 64 sequences of one token over up to 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 of 33
-// rows over up to 2000 (32 heads) 218 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 206 us, 580 TFLOP/s;
-// one of 34 rows over 600 (32 heads) 15.6 us.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
+// Bound by reading the keys and values, beyond the L2 as often as a head has blocks of rows, and by latency in small calls.  Replayed from
+// a graph: 64 sequences of one token over up to 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 of 33 rows over up to 2000
+// (32 heads) 219 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 208 us, 570 TFLOP/s, 981 MB read for 385 of keys and
+// values; one of 34 rows over 600 (32 heads) 15.9 us, 62 % of it waiting.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
 // row's scores: the softmax, and the rescaling of the transposed sums, need no exchange but two swaps.  Weights are rounded to
 // bfloat16 for the second product, each by at most 2^-8 of itself (a product in float32 has an eighth of the rate: 141 and 1153
 // TFLOP/s), and their sum is that of the rounded ones: an output is a mean of the values with weights that far from the exact ones.
@@ -93,8 +93,9 @@ __device__ __forceinline__ SeqTiles seq_tiles(const AttentionJob& p, int q, int 
   return s;
 }
 
-// Shares of up to this cost go to one workgroup per CU, more of them to two: 4 sequences of 32 heads, 10 tiles a share: 28.9 us with
-// one, 30.8 us with two; 24 sequences of one key/value head, 31 tiles a share: 86 us and 75 us.
+// Shares of up to this cost go to one workgroup per CU, more of them to two.  With one and with two, at shares of 12, 16, 20 and 24: three
+// sequences of 32 heads of their own 28.1 / 30.9, 34.0 / 35.1, 48.6 / 47.9 and 55.5 / 55.1 us; 12 sequences of 6 rows, one key/value head, 43.3 /
+// 46.3, 46.9 / 47.5, 55.7 / 49.8 and 59.4 / 53.6.  Where heads are shared by 8 and there are many rows, two are faster from 12 on (46.4 / 41.8).
 constexpr uint64_t kFewCost = 20;
 
 // What a workgroup that ends inside a unit leaves: see the join below.
@@ -369,7 +370,8 @@ __device__ __forceinline__ void add_left_out(AttentionTile<BF16, DP, MQ, WK>& x,
 // not what stands behind the elements of a key (copies of its last 16 bytes).  Where segments with such keys have sums that are
 // not finite, the workgroup goes through its share a second time, CAREFULLY: in every tile that has landed, zeros take the place of what
 // is behind the elements and of the values that are not finite of all that is not a cached token.  (In every pass over a tile with rows
-// of the tree: 41 -> 46 us for 64 sequences of 100 tokens.)
+// of the tree: 41 -> 46 us for 64 sequences of 100 tokens.  Key by key for every row of such a wave: 45 us -> 16 ms with one infinity among
+// 16 sequences of up to 3000 tokens; so: 32 of 45 rows over up to 4000 212 -> 443 us.)
 template <bool BF16, int DP, int MQ, int WK>
 __device__ __forceinline__ void clean_tile(lds_u8* cur, uint64_t cached, int last_word) {
   typedef AttentionShape<BF16, DP, MQ, WK> S;
@@ -910,8 +912,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionJob p, Att
 // float32 heads of more than 128 elements (two buffers of their tiles do not fit a CU's memory with 64 keys): units of 16 query
 // rows, four to a wave, straight from memory.  16 lanes take a key, four keys at once, 16 elements of the head per lane; the
 // waves read the same keys, three of them from the cache.  Bound by the latency of a key's loads, one key ahead, and the vector
-// units: 4 sequences of up to 1000 tokens, 32 query heads on 8 of 192, 32 rows: 323 us, 8.3 TFLOP/s; one of 20000 tokens, 8 query
-// heads on one of 256: 118 us.  (A workgroup per row, unsplit: 1.02 ms and 12.1 ms.)
+// units: 4 sequences of up to 1000 tokens, 32 query heads on 8 of 192, 32 rows: 320 us, 8.3 TFLOP/s; one of 20000 tokens, 8 query
+// heads on one of 256: 117 us.  (A workgroup per row, unsplit: 1.02 ms and 12.1 ms.)
 constexpr int kWideRows = 16;   // query rows of a unit
 __global__ __launch_bounds__(256, 2) void attention_wide_kernel(AttentionJob p, AttentionSpace ws) {
   constexpr int BM = kWideRows, DP = 256;
