@@ -9,7 +9,7 @@
 //
 // Bound by reading the keys and values, beyond the L2 as often as a head has blocks of rows, and by latency in small calls.  Replayed from
 // a graph: 64 sequences of one token over up to 8000 (8 heads of 128, 64 query heads) 200 us, 5.0 TB/s; 48 of 33 rows over up to 2000
-// (32 heads) 219 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 208 us, 570 TFLOP/s, 981 MB read for 385 of keys and
+// (32 heads) 219 us, 4.7 TB/s; 32 of 45 rows over up to 4000 (8 heads, 64 query heads) 208 us, 570 TFLOP/s, 980 MB read for 385 of keys and
 // values; one of 34 rows over 600 (32 heads) 15.9 us, 62 % of it waiting.  Scores are computed transposed, keys times queries, so that a lane's registers hold one query
 // row's scores: the softmax, and the rescaling of the transposed sums, need no exchange but two swaps.  Weights are rounded to
 // bfloat16 for the second product, each by at most 2^-8 of itself (a product in float32 has an eighth of the rate: 141 and 1153
