@@ -438,6 +438,79 @@ spec_status_t spec_verify_tree(const void* logits, int32_t logits_dtype, const i
                                int32_t* out_tokens, int32_t* n_out, int32_t* path_row, int32_t* accept_all,
                                int32_t* counts_out, uint32_t* seen_out, void* hip_stream);
 
+/* ---- rotation and norms of heads, and a cache of four bits ----------------------------------------------------
+ * Table of a rotation: the pair i of a head (i < rot_dim / 2) at position x is turned by the angle whose cosine and sine are
+ * cos[x][i] and sin[x][i]:  (a, b) -> (a cos - b sin, b cos + a sin).  The pair is the elements i and i + rot_dim / 2, or with
+ * pairs = 1 the elements 2 i and 2 i + 1; elements from rot_dim on stay as they are.
+ *   cos, sin    dev [n_pos, rot_dim / 2] float32, 16-byte aligned
+ *   rot_dim     multiple of 16 (SPEC_BF16) or 8 (SPEC_F32), at most head_dim */
+typedef struct {
+  const float* cos;
+  const float* sin;
+  int32_t n_pos, rot_dim, pairs;
+} spec_rotation_t;
+
+/* NORMS AND ROTATION of the rows' queries and keys in one pass.  Per head of D elements, with weight given:
+ *     x = x * (1 / sqrt(mean(x^2) + eps)) * weight
+ * (the mean and its root in 64 bits, then a float32 factor), then the rotation; every other operation in float32, rounded by itself,
+ * and one rounding to dtype.
+ *   q, q_out    rows of q_heads;  k, k_out rows of kv_heads, or both NULL (kv_heads is then not looked at)
+ *   pos         dev [batch, M + 1]: the rows' positions, those below 0 do not exist; or NULL, and
+ *   ctx_len, node_depth, n_nodes  dev [batch], [batch, M], [batch]: row 0 stands at ctx_len[q], row 1 + i at ctx_len[q] +
+ *                     node_depth[q][i]; n_nodes as for spec_tree_attention (with pos, n_nodes is not looked at)
+ *   rotation    host, NULL: norms only;  q_weight, k_weight  dev [head_dim] float32, 16-byte aligned, NULL: no norm
+ * Rows that do not exist, and rows whose position is outside the table, are not written.  q_out may be q and k_out k, row for row;
+ * else the outputs overlap nothing, and no two of their rows share memory (refused as for spec_tree_attention's out).
+ * batch * (M + 1) <= 2^25, heads <= 65535. */
+spec_status_t spec_rotate_rows(const spec_rows_t* q, const spec_rows_t* k, const spec_rows_t* q_out, const spec_rows_t* k_out,
+                               int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                               const int32_t* pos, const int32_t* ctx_len, const int32_t* node_depth, const int32_t* n_nodes,
+                               const spec_rotation_t* rotation, const float* q_weight, const float* k_weight, double eps,
+                               void* hip_stream);
+
+/* APPEND: spec_cache_store with the keys' norm and rotation on the way, as spec_rotate_rows does them; values are copied.
+ *   pos         dev [count] int32: the entries' positions (spec_cache_extend's); may be NULL without a rotation
+ *   k_weight    dev [layers, head_dim] float32, NULL: no norm
+ * Entries without a slot, with a source row outside [0, rows) or (with a rotation) a position outside the table are skipped; the
+ * slots of one call are distinct.  k_new and v_new do not overlap the cache.  count <= 2^25. */
+spec_status_t spec_cache_append(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_cache_t* cache,
+                                int64_t cache_layer_stride, int32_t layers, int32_t rows, int32_t kv_heads, int32_t head_dim,
+                                int32_t dtype, const int32_t* slot, const int32_t* src_row, const int32_t* pos, int32_t count,
+                                const spec_rotation_t* rotation, const float* k_weight, double eps, void* hip_stream);
+
+/* A paged cache of four bits an element: 17 bytes for 32 elements of a head.  Such a group has a scale byte s and 32 codes; a code's
+ * lowest three bits stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6, the highest for the sign, and a value is that amount times 2^(s - 127)
+ * (s = 255: not a number; 2^128 and more, which no append writes: infinite).  Bfloat16 holds every value as it is.  Token t of sequence q lies in block b and slot as in spec_cache_t;
+ * element (h, d) is in byte d / 2 of the codes at block_stride * b + slot_stride * slot + head_stride * h, even elements in its low
+ * half, and group d / 32's scale at the same place of the scales by their strides.  Strides in bytes; rows of codes start on multiples
+ * of 16 bytes, scales anywhere.  head_dim is a multiple of 32, at most 256. */
+typedef struct {
+  const void* k; /* dev */
+  const void* v; /* dev */
+  const uint8_t* k_scale; /* dev */
+  const uint8_t* v_scale; /* dev */
+  int64_t block_stride, slot_stride, head_stride;
+  int64_t scale_block_stride, scale_slot_stride, scale_head_stride;
+  int32_t n_blocks, block_size; /* n_blocks * block_size <= 2^30 */
+} spec_packed_t;
+
+/* APPEND to a cache of four bits: spec_cache_append of bfloat16 rows, what would be rounded to bfloat16 last is packed instead.  A group's
+ * scale is the smallest 2^e, -125 <= e <= 125, with (its largest amount) <= 7 * 2^e; every element is rounded to the nearest value, of
+ * two as near to the one with the even code, what is above 6 * 2^e to that.  A group with an infinity or NaN gets scale 255. */
+spec_status_t spec_packed_append(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_packed_t* cache,
+                                 int64_t cache_layer_stride, int64_t scale_layer_stride, int32_t layers, int32_t rows,
+                                 int32_t kv_heads, int32_t head_dim, const int32_t* slot, const int32_t* src_row,
+                                 const int32_t* pos, int32_t count, const spec_rotation_t* rotation, const float* k_weight,
+                                 double eps, void* hip_stream);
+
+/* LOAD of tokens of a cache of four bits as bfloat16 rows (a prefix that requests share, for the base model's own attention over
+ * their prompts):  out[l][t] = cache[l][slot[t]]  for t < count.
+ *   k_out, v_out  rows of kv_heads, the same strides; seq_stride is the distance of two layers; no two rows share memory
+ * Rows of entries whose slot is outside [0, n_blocks * block_size) are not written; slots may repeat. */
+spec_status_t spec_packed_load(const spec_packed_t* cache, int64_t cache_layer_stride, int64_t scale_layer_stride, int32_t layers,
+                               int32_t kv_heads, int32_t head_dim, const int32_t* slot, int32_t count, const spec_rows_t* k_out,
+                               const spec_rows_t* v_out, void* hip_stream);
+
 /* Measurement aid, not a step of the method: one launch of a plain copy kernel that
  * reads `bytes` from src (dev) and writes them to dst (dev; must not overlap src).  Its HBM
  * traffic is known exactly, which calibrates the memory-traffic hardware counters that

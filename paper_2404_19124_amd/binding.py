@@ -23,7 +23,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecdraf
 
 EXPORTS = ["spec_create", "spec_destroy", "spec_draft", "spec_draft_static", "spec_draft_dynamic", "spec_verify", "spec_verify_dynamic", "spec_head_logp", "spec_model_scalars",
            "spec_profile_enable", "spec_profile_read", "spec_copy_probe", "spec_tree_metadata", "spec_advance", "spec_tree_attention", "spec_tree_attention_workspace", "spec_cache_extend",
-           "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
+           "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_rotate_rows", "spec_cache_append", "spec_packed_append", "spec_packed_load", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
 
 
 class SpecError(RuntimeError):
@@ -55,6 +55,16 @@ class spec_rows_t(C.Structure):
 class spec_cache_t(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("block_stride", C.c_int64), ("slot_stride", C.c_int64),
                 ("head_stride", C.c_int64), ("n_blocks", C.c_int32), ("block_size", C.c_int32)]
+
+
+class spec_rotation_t(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("pairs", C.c_int32)]
+
+
+class spec_packed_t(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("k", "v", "k_scale", "v_scale")] + [
+        (name, C.c_int64) for name in ("block_stride", "slot_stride", "head_stride", "scale_block_stride", "scale_slot_stride",
+                                       "scale_head_stride")] + [("n_blocks", C.c_int32), ("block_size", C.c_int32)]
 
 
 class spec_penalties_t(C.Structure):
@@ -138,6 +148,15 @@ def lib() -> C.CDLL:
         l.spec_penalize.argtypes = [ptr] + [i32] * 4 + [pen] + [ptr] * 5
         l.spec_verify_tree.restype = C.c_int
         l.spec_verify_tree.argtypes = [ptr, i32] + [ptr] * 6 + [pen] + [i32] * 5 + [ptr] * 10
+        turn, packed, dbl = C.POINTER(spec_rotation_t), C.POINTER(spec_packed_t), C.c_double
+        l.spec_rotate_rows.restype = C.c_int
+        l.spec_rotate_rows.argtypes = [rows] * 4 + [i32] * 6 + [ptr] * 4 + [turn, ptr, ptr, dbl, ptr]
+        l.spec_cache_append.restype = C.c_int
+        l.spec_cache_append.argtypes = [rows, rows, cache, C.c_int64] + [i32] * 5 + [ptr] * 3 + [i32, turn, ptr, dbl, ptr]
+        l.spec_packed_append.restype = C.c_int
+        l.spec_packed_append.argtypes = [rows, rows, packed, C.c_int64, C.c_int64] + [i32] * 4 + [ptr] * 3 + [i32, turn, ptr, dbl, ptr]
+        l.spec_packed_load.restype = C.c_int
+        l.spec_packed_load.argtypes = [packed, C.c_int64, C.c_int64] + [i32] * 3 + [ptr, i32, rows, rows, ptr]
         l.spec_copy_probe.restype = C.c_int
         l.spec_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         l.spec_last_error.restype = C.c_char_p
@@ -162,7 +181,8 @@ def _native():
                                "fallback path") from e
         at = [C.cast(f, C.c_void_p).value for f in (l.spec_verify, l.spec_verify_dynamic, l.spec_advance, l.spec_tree_metadata,
                                                     l.spec_draft, l.spec_tree_attention, l.spec_cache_extend, l.spec_cache_store,
-                                                    l.spec_penalize, l.spec_verify_tree)]
+                                                    l.spec_penalize, l.spec_verify_tree, l.spec_rotate_rows, l.spec_cache_append,
+                                                    l.spec_packed_append, l.spec_packed_load)]
         _call.bind(*at[:5], lambda stream: _stream_ptr(stream), *at[5:])
         _fast = _call
     return _fast
@@ -816,6 +836,196 @@ def spec_verify_tree(logits: torch.Tensor, cand_tokens: torch.Tensor, cand_node:
         _ptr(node_parent) or None, _ptr(n_nodes), C.byref(pen) if pen is not None else None, b, R - 1, Bc, n, V, _ptr(greedy),
         _ptr(accept_len), _ptr(best_cand), _ptr(out_tokens), _ptr(n_out), _ptr(path_row), _ptr(accept_all),
         pen.counts if update else None, pen.seen if update else None, _stream_ptr(stream)))
+
+
+# ---- rotation and norms of heads, and a cache of four bits ----
+
+def _rotation(cos, sin, pairs, stream) -> Optional[spec_rotation_t]:
+    if cos is None and sin is None:
+        return None
+    if not isinstance(cos, torch.Tensor) or cos.dim() != 2 or sin is None:
+        raise ValueError("cos and sin must be [positions, half of the rotated elements] tensors, both or neither")
+    n, half = cos.shape
+    _require(cos, "cos", torch.float32)
+    _require(sin, "sin", torch.float32, (n, half))
+    _here(stream, cos=cos, sin=sin)
+    return spec_rotation_t(_ptr(cos), _ptr(sin), n, 2 * half, int(bool(pairs)))
+
+
+def _by(x):
+    return C.byref(x) if x is not None else None
+
+
+def spec_rotate_rows(q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor],
+                     cos: Optional[torch.Tensor], sin: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None,
+                     ctx_len: Optional[torch.Tensor] = None, node_depth: Optional[torch.Tensor] = None,
+                     n_nodes: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, pairs: bool = False, stream=None) -> None:
+    """Enqueues norms and the position rotation of R rows' queries and keys per sequence, in one pass.
+
+    q, q_out [batch, R, q_heads, head_dim], k, k_out [batch, R, kv_heads, head_dim] (or both None): strides as for
+    spec_tree_attention; q_out may be q, and k_out k.  cos, sin [positions, half] float32: the first 2 * half elements of a head are
+    turned, i with i + half (pairs: 2 i with 2 i + 1); None: norms only.  Positions: pos [batch, R] int32 (below 0: no row), or
+    ctx_len [batch] with node_depth [batch, R - 1] and n_nodes [batch] as of a tree's rows.  q_weight, k_weight [head_dim] float32 of a
+    norm by the root of the mean square.  Rows that do not exist, or whose position is outside the table, are not written."""
+    if _CHECK_DEVICE and _done((_fast or _native()).rotate_rows(
+            q, k, q_out, k_out, cos, sin, pos, ctx_len, node_depth, n_nodes, q_weight, k_weight, eps, pairs, stream)):
+        return
+    code = _float_code(q, "q", (4,))
+    b, R, H, D = q.shape
+    if R < 1:
+        raise ValueError("q needs a row per sequence")
+    sq, so = _strided(q, "q", q.dtype, (b, R, H, D)), _strided(q_out, "q_out", q.dtype, (b, R, H, D))
+    _written(q_out, "q_out")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    KH = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a [batch, R, kv_heads, head_dim] tensor")
+        KH = int(k.shape[2])
+        sk, sko = _strided(k, "k", q.dtype, (b, R, KH, D)), _strided(k_out, "k_out", q.dtype, (b, R, KH, D))
+        _written(k_out, "k_out")
+    i32, f32 = torch.int32, torch.float32
+    _require(pos, "pos", i32, (b, R), optional=True)
+    _require(ctx_len, "ctx_len", i32, (b,), optional=True)
+    _require(node_depth, "node_depth", i32, (b, R - 1), optional=True)
+    _require(n_nodes, "n_nodes", i32, (b,), optional=True)
+    _require(q_weight, "q_weight", f32, (D,), optional=True)
+    _require(k_weight, "k_weight", f32, (D,), optional=True)
+    turn = _rotation(cos, sin, pairs, stream)
+    _here(stream, q=q, k=k, q_out=q_out, k_out=k_out, pos=pos, ctx_len=ctx_len, node_depth=node_depth, n_nodes=n_nodes, q_weight=q_weight,
+          k_weight=k_weight)
+    _check(lib().spec_rotate_rows(
+        C.byref(spec_rows_t(_ptr(q), *sq)), C.byref(spec_rows_t(_ptr(k), *sk)) if KH else None, C.byref(spec_rows_t(_ptr(q_out), *so)),
+        C.byref(spec_rows_t(_ptr(k_out), *sko)) if KH else None, b, R - 1, H, KH, D, code, _ptr(pos), _ptr(ctx_len), _ptr(node_depth) or None,
+        _ptr(n_nodes), _by(turn), _ptr(q_weight), _ptr(k_weight), float(eps), _stream_ptr(stream)))
+
+
+def _append_rows(k_new, v_new, dtype, L, KH, D):
+    """Rows, heads and strides of new keys and values with a first dimension of layers."""
+    if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4:
+        raise ValueError("k_new must be a [rows, kv_heads, head_dim] tensor, with layers first where the cache has them")
+    rows = int(k_new.shape[1])
+    sk, sv = _strided(k_new, "k_new", dtype, (L, rows, KH, D)), _strided(v_new, "v_new", dtype, (L, rows, KH, D))
+    if sk != sv:
+        raise ValueError("k_new and v_new must have the same strides")
+    return rows, sk
+
+
+def _entries(slot, src_row, pos, k_weight, L, D) -> int:
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
+        raise ValueError("slot must be a [count] tensor")
+    count = int(slot.shape[0])
+    _require(slot, "slot", torch.int32, (count,))
+    _require(src_row, "src_row", torch.int32, (count,), optional=True)
+    _require(pos, "pos", torch.int32, (count,), optional=True)
+    _require(k_weight, "k_weight", torch.float32, (L, D), optional=True)
+    return count
+
+
+def _with_layers(single: bool, *tensors):
+    return [t.unsqueeze(0) if single and isinstance(t, torch.Tensor) else t for t in tensors]
+
+
+def spec_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      src_row: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                      sin: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                      pairs: bool = False, stream=None) -> None:
+    """Enqueues spec_cache_store with the keys' norm and rotation on the way (as spec_rotate_rows does them).
+
+    Tensors as for spec_cache_store; pos [count] int32: the entries' positions; cos, sin, pairs as for spec_rotate_rows; k_weight
+    [head_dim], or [layers, head_dim] where the cache has layers, float32.  Entries without a slot, or whose position is outside the
+    table, are skipped."""
+    if _CHECK_DEVICE and _done((_fast or _native()).cache_append(
+            k_new, v_new, slot, k_cache, v_cache, src_row, pos, cos, sin, k_weight, eps, pairs, stream)):
+        return
+    code = _float_code(k_cache, "k_cache", (4, 5))
+    k_new, v_new, k_cache, v_cache, k_weight = _with_layers(k_cache.dim() == 4, k_new, v_new, k_cache, v_cache, k_weight)
+    L, n_blocks, page, KH, D = k_cache.shape
+    rows, sk = _append_rows(k_new, v_new, k_cache.dtype, L, KH, D)
+    ck = _strided(k_cache, "k_cache", k_cache.dtype, (L, n_blocks, page, KH, D))
+    cv = _strided(v_cache, "v_cache", k_cache.dtype, (L, n_blocks, page, KH, D))
+    if ck != cv:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    _written(k_cache, "k_cache")
+    _written(v_cache, "v_cache")
+    count = _entries(slot, src_row, pos, k_weight, L, D)
+    turn = _rotation(cos, sin, pairs, stream)
+    _here(stream, k_new=k_new, v_new=v_new, k_cache=k_cache, v_cache=v_cache, slot=slot, src_row=src_row, pos=pos, k_weight=k_weight)
+    _check(lib().spec_cache_append(C.byref(spec_rows_t(_ptr(k_new), *sk)), C.byref(spec_rows_t(_ptr(v_new), *sk)),
+                                   C.byref(spec_cache_t(_ptr(k_cache), _ptr(v_cache), *ck[1:], n_blocks, page)), ck[0], L, rows, KH, D,
+                                   code, _ptr(slot), _ptr(src_row), _ptr(pos), count, _by(turn), _ptr(k_weight), float(eps),
+                                   _stream_ptr(stream)))
+
+
+def _packed(k_cache, v_cache, k_scale, v_scale, stream):
+    """(cache, layer strides, (L, heads, head_dim)) of a cache of four bits with a first dimension of layers."""
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 5:
+        raise ValueError("k_cache must be a [n_blocks, block_size, kv_heads, head_dim / 2] tensor, or one with layers first")
+    L, n_blocks, page, KH, half = k_cache.shape
+    if half % 16:
+        raise ValueError("head_dim must be a multiple of 32: k_cache has %d bytes per head" % half)
+    ck, cv = (_strided(t, n, torch.uint8, k_cache.shape) for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache")))
+    shape = (L, n_blocks, page, KH, half // 16)
+    sk, sv = (_strided(t, n, torch.uint8, shape) for t, n in ((k_scale, "k_scale"), (v_scale, "v_scale")))
+    if ck != cv or sk != sv:
+        raise ValueError("k_cache and v_cache, and k_scale and v_scale, must have the same strides")
+    _here(stream, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
+    at = spec_packed_t(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), *ck[1:], *sk[1:], n_blocks, page)
+    return at, ck[0], sk[0], (L, KH, 2 * half)
+
+
+def spec_packed_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                       k_scale: torch.Tensor, v_scale: torch.Tensor, src_row: Optional[torch.Tensor] = None,
+                       pos: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                       k_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, pairs: bool = False, stream=None) -> None:
+    """Enqueues spec_cache_append of bfloat16 rows into a cache of four bits.
+
+    One layer: k_new, v_new [rows, kv_heads, head_dim]; k_cache, v_cache [n_blocks, block_size, kv_heads, head_dim / 2] uint8, rows on 16
+    bytes; k_scale, v_scale [n_blocks, block_size, kv_heads, head_dim / 32] uint8: any strides but along the last dimension, the same in
+    k_* and v_*.  Several layers at once: a first dimension of layers in all six.  The others as for spec_cache_append."""
+    if _CHECK_DEVICE and _done((_fast or _native()).packed_append(
+            k_new, v_new, slot, k_cache, v_cache, k_scale, v_scale, src_row, pos, cos, sin, k_weight, eps, pairs, stream)):
+        return
+    if isinstance(k_cache, torch.Tensor):
+        k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_weight = _with_layers(
+            k_cache.dim() == 4, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_weight)
+    at, layer, scale_layer, (L, KH, D) = _packed(k_cache, v_cache, k_scale, v_scale, stream)
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+        _written(t, name)
+    rows, sk = _append_rows(k_new, v_new, torch.bfloat16, L, KH, D)
+    count = _entries(slot, src_row, pos, k_weight, L, D)
+    turn = _rotation(cos, sin, pairs, stream)
+    _here(stream, k_new=k_new, v_new=v_new, slot=slot, src_row=src_row, pos=pos, k_weight=k_weight)
+    _check(lib().spec_packed_append(C.byref(spec_rows_t(_ptr(k_new), *sk)), C.byref(spec_rows_t(_ptr(v_new), *sk)), C.byref(at), layer,
+                                    scale_layer, L, rows, KH, D, _ptr(slot), _ptr(src_row), _ptr(pos), count, _by(turn), _ptr(k_weight),
+                                    float(eps), _stream_ptr(stream)))
+
+
+def spec_packed_load(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, slot: torch.Tensor,
+                     k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
+    """Enqueues the load of tokens of a cache of four bits as bfloat16 rows: slot[t] into row t of k_out, v_out.
+
+    Caches as for spec_packed_append; slot [count] int32; k_out, v_out [count, kv_heads, head_dim], or with layers first, any strides
+    but along head_dim, rows on 16 bytes, the same in both."""
+    if _CHECK_DEVICE and _done((_fast or _native()).packed_load(k_cache, v_cache, k_scale, v_scale, slot, k_out, v_out, stream)):
+        return
+    if isinstance(k_cache, torch.Tensor):
+        k_cache, v_cache, k_scale, v_scale, k_out, v_out = _with_layers(k_cache.dim() == 4, k_cache, v_cache, k_scale, v_scale, k_out, v_out)
+    at, layer, scale_layer, (L, KH, D) = _packed(k_cache, v_cache, k_scale, v_scale, stream)
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
+        raise ValueError("slot must be a [count] tensor")
+    count = int(slot.shape[0])
+    _require(slot, "slot", torch.int32, (count,))
+    so, sv = (_strided(t, n, torch.bfloat16, (L, count, KH, D)) for t, n in ((k_out, "k_out"), (v_out, "v_out")))
+    if so != sv:
+        raise ValueError("k_out and v_out must have the same strides")
+    _written(k_out, "k_out")
+    _written(v_out, "v_out")
+    _here(stream, slot=slot, k_out=k_out, v_out=v_out)
+    _check(lib().spec_packed_load(C.byref(at), layer, scale_layer, L, KH, D, _ptr(slot), count, C.byref(spec_rows_t(_ptr(k_out), *so)),
+                                  C.byref(spec_rows_t(_ptr(v_out), *so)), _stream_ptr(stream)))
 
 
 def spec_plan_contraction(rows: int, k: int, n_head: int, k_top: int, n_proj: int, n_cu: int = 256) -> dict:

@@ -36,6 +36,7 @@ SOURCES = [
     "kernels_tree_attention.hip",
     "kernels_cache.hip",
     "kernels_rows.hip",
+    "kernels_heads.hip",
     "rows_lib.hip",
 ]
 

@@ -30,6 +30,10 @@ decltype(&spec_cache_extend) f_cache_extend;
 decltype(&spec_cache_store) f_cache_store;
 decltype(&spec_penalize) f_penalize;
 decltype(&spec_verify_tree) f_verify_tree;
+decltype(&spec_rotate_rows) f_rotate_rows;
+decltype(&spec_cache_append) f_cache_append;
+decltype(&spec_packed_append) f_packed_append;
+decltype(&spec_packed_load) f_packed_load;
 PyObject* f_stream;   // the binding's _stream_ptr
 
 const at::Tensor* tensor(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
@@ -449,12 +453,216 @@ PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// cos, sin (both None: no rotation), pairs; false: not the usual case
+struct Turn {
+  spec_rotation_t r;
+  const spec_rotation_t* at = nullptr;
+};
+bool rotation(const Rows& on, PyObject* cos, PyObject* sin, PyObject* pairs, Turn* t) {
+  if (!PyBool_Check(pairs) || (cos == Py_None) != (sin == Py_None)) return false;
+  if (cos == Py_None) return true;
+  const int64_t n = size_of(cos, 2, 0), half = size_of(cos, 2, 1);
+  float *c, *s;
+  if (n < 0 || half < 0 || half > INT32_MAX / 2 || !on.in(cos, at::kFloat, {n, half}, &c) || !on.in(sin, at::kFloat, {n, half}, &s)) return false;
+  t->r = {c, s, (int32_t)n, (int32_t)(2 * half), pairs == Py_True};
+  t->at = &t->r;
+  return true;
+}
+
+bool double_of(PyObject* o, double* x) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *x = PyFloat_AS_DOUBLE(o);
+  return true;
+}
+
+// q, k, q_out, k_out, cos, sin, pos, ctx_len, node_depth, n_nodes, q_weight, k_weight, eps, pairs, stream
+PyObject* rotate_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 15 || (a[1] == Py_None) != (a[3] == Py_None)) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    int64_t d[4], sq[3], sqo[3], sk[3], sko[3], KH = 0;
+    int32_t code, *pos, *ctx, *depth, *count;
+    at::ScalarType dt;
+    void *at[4], *stream;
+    float *qw, *kw;
+    double eps;
+    Turn turn;
+    const bool keys = a[1] != Py_None;
+    if (!floats(a[0], 4, d, &code, &dt) || d[1] < 1 || !on.strided(a[0], dt, {d[0], d[1], d[2], d[3]}, sq, &at[0]) ||
+        !on.strided(a[2], dt, {d[0], d[1], d[2], d[3]}, sqo, &at[1], true) || !rotation(on, a[4], a[5], a[13], &turn) || !double_of(a[12], &eps))
+      Py_RETURN_NONE;
+    if (keys) {
+      KH = size_of(a[1], 4, 2);
+      if (KH < 1 || !on.strided(a[1], dt, {d[0], d[1], KH, d[3]}, sk, &at[2]) || !on.strided(a[3], dt, {d[0], d[1], KH, d[3]}, sko, &at[3], true))
+        Py_RETURN_NONE;
+    }
+    if (!on.maybe(a[6], at::kInt, {d[0], d[1]}, &pos) || !on.maybe(a[7], at::kInt, {d[0]}, &ctx) ||
+        !on.maybe(a[8], at::kInt, {d[0], d[1] - 1}, &depth) || !on.maybe(a[9], at::kInt, {d[0]}, &count) ||
+        !on.maybe(a[10], at::kFloat, {d[3]}, &qw) || !on.maybe(a[11], at::kFloat, {d[3]}, &kw) || !on.here(a[14]))
+      Py_RETURN_NONE;
+    const spec_rows_t q = {at[0], sq[0], sq[1], sq[2]}, qo = {at[1], sqo[0], sqo[1], sqo[2]};
+    spec_rows_t k, ko;
+    if (keys) k = {at[2], sk[0], sk[1], sk[2]}, ko = {at[3], sko[0], sko[1], sko[2]};
+    if (!stream_of(a[14], &stream)) return nullptr;
+    return status_of([&] {
+      return f_rotate_rows(&q, keys ? &k : nullptr, &qo, keys ? &ko : nullptr, (int32_t)d[0], (int32_t)d[1] - 1, (int32_t)d[2], (int32_t)KH,
+                           (int32_t)d[3], code, pos, ctx, depth, count, turn.at, qw, kw, eps, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
+// What is appended: new rows, entries, rotation and norm; layers first, or (single) one layer
+struct Appended {
+  spec_rows_t k, v;
+  int64_t rows, count;
+  int32_t *slot, *src, *pos;
+  float* weight;
+  double eps;
+  Turn turn;
+};
+// a: k_new, v_new, slot; b: src_row, pos, cos, sin, k_weight, eps, pairs
+bool appended(const Rows& on, PyObject* const* a, PyObject* const* b, bool single, at::ScalarType dt, int64_t L, int64_t H, int64_t D, Appended* x) {
+  int64_t sk[3] = {0}, sv[3] = {0};
+  void *k, *v;
+  x->rows = size_of(a[0], single ? 3 : 4, single ? 0 : 1);
+  x->count = size_of(a[2], 1, 0);
+  if (x->rows < 0 || x->count < 0) return false;
+  if (single) {
+    if (!on.strided(a[0], dt, {x->rows, H, D}, sk + 1, &k) || !on.strided(a[1], dt, {x->rows, H, D}, sv + 1, &v)) return false;
+  } else if (!on.strided(a[0], dt, {L, x->rows, H, D}, sk, &k) || !on.strided(a[1], dt, {L, x->rows, H, D}, sv, &v)) {
+    return false;
+  }
+  for (int i = 0; i < 3; ++i)
+    if (sk[i] != sv[i]) return false;
+  x->k = {k, sk[0], sk[1], sk[2]}, x->v = {v, sv[0], sv[1], sv[2]};
+  return on.in(a[2], at::kInt, {x->count}, &x->slot) && on.maybe(b[0], at::kInt, {x->count}, &x->src) && on.maybe(b[1], at::kInt, {x->count}, &x->pos) &&
+         rotation(on, b[2], b[3], b[6], &x->turn) && (single ? on.maybe(b[4], at::kFloat, {D}, &x->weight) : on.maybe(b[4], at::kFloat, {L, D}, &x->weight)) &&
+         double_of(b[5], &x->eps);
+}
+
+// k_new, v_new, slot, k_cache, v_cache, src_row, pos, cos, sin, k_weight, eps, pairs, stream
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 13) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    int64_t c[5] = {1}, ck[4] = {0}, cv[4] = {0};
+    int32_t code;
+    at::ScalarType dt;
+    void *k, *v, *stream;
+    Appended x;
+    const bool single = floats(a[3], 4, c + 1, &code, &dt);
+    if (single) {
+      if (!on.strided(a[3], dt, {c[1], c[2], c[3], c[4]}, ck + 1, &k, true) || !on.strided(a[4], dt, {c[1], c[2], c[3], c[4]}, cv + 1, &v, true)) Py_RETURN_NONE;
+    } else if (!floats(a[3], 5, c, &code, &dt) || !on.strided(a[3], dt, {c[0], c[1], c[2], c[3], c[4]}, ck, &k, true) ||
+               !on.strided(a[4], dt, {c[0], c[1], c[2], c[3], c[4]}, cv, &v, true)) {
+      Py_RETURN_NONE;
+    }
+    for (int i = 0; i < 4; ++i)
+      if (ck[i] != cv[i]) Py_RETURN_NONE;
+    if (!appended(on, a, a + 5, single, dt, c[0], c[3], c[4], &x) || !on.here(a[12])) Py_RETURN_NONE;
+    const spec_cache_t cache = {k, v, ck[1], ck[2], ck[3], (int32_t)c[1], (int32_t)c[2]};
+    if (!stream_of(a[12], &stream)) return nullptr;
+    return status_of([&] {
+      return f_cache_append(&x.k, &x.v, &cache, ck[0], (int32_t)c[0], (int32_t)x.rows, (int32_t)c[3], (int32_t)c[4], code, x.slot, x.src, x.pos,
+                            (int32_t)x.count, x.turn.at, x.weight, x.eps, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
+// k_cache, v_cache, k_scale, v_scale of four bits; layers first, or one layer
+struct Packed {
+  spec_packed_t at;
+  int64_t L = 1, blocks, page, H, D, layer = 0, scale_layer = 0;
+  bool single;
+};
+bool packed(const Rows& on, PyObject* const* a, bool written, Packed* x) {
+  const at::Tensor* t = tensor(a[0]);
+  if (!t || (t->dim() != 4 && t->dim() != 5)) return false;
+  x->single = t->dim() == 4;
+  const int64_t dim = t->dim();
+  for (int64_t i = 0; i < dim; ++i)
+    if (t->size(i) > INT32_MAX / 2) return false;
+  if (!x->single) x->L = t->size(0);
+  x->blocks = t->size(dim - 4), x->page = t->size(dim - 3), x->H = t->size(dim - 2);
+  const int64_t half = t->size(dim - 1), groups = half / 16;
+  if (half % 16) return false;
+  x->D = 2 * half;
+  int64_t s[4][4] = {};
+  void* at[4];
+  for (int i = 0; i < 4; ++i) {
+    const int64_t last = i < 2 ? half : groups;
+    if (x->single ? !on.strided(a[i], at::kByte, {x->blocks, x->page, x->H, last}, s[i] + 1, &at[i], written)
+                  : !on.strided(a[i], at::kByte, {x->L, x->blocks, x->page, x->H, last}, s[i], &at[i], written))
+      return false;
+  }
+  for (int i = 0; i < 4; ++i)
+    if (s[0][i] != s[1][i] || s[2][i] != s[3][i]) return false;
+  x->at = {at[0], at[1], static_cast<const uint8_t*>(at[2]), static_cast<const uint8_t*>(at[3]), s[0][1], s[0][2], s[0][3], s[2][1], s[2][2], s[2][3],
+           (int32_t)x->blocks, (int32_t)x->page};
+  x->layer = s[0][0], x->scale_layer = s[2][0];
+  return true;
+}
+
+// k_new, v_new, slot, k_cache, v_cache, k_scale, v_scale, src_row, pos, cos, sin, k_weight, eps, pairs, stream
+PyObject* packed_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 15) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    Packed c;
+    Appended x;
+    void* stream;
+    if (!packed(on, a + 3, true, &c) || !appended(on, a, a + 7, c.single, at::kBFloat16, c.L, c.H, c.D, &x) || !on.here(a[14])) Py_RETURN_NONE;
+    if (!stream_of(a[14], &stream)) return nullptr;
+    return status_of([&] {
+      return f_packed_append(&x.k, &x.v, &c.at, c.layer, c.scale_layer, (int32_t)c.L, (int32_t)x.rows, (int32_t)c.H, (int32_t)c.D, x.slot, x.src, x.pos,
+                             (int32_t)x.count, x.turn.at, x.weight, x.eps, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
+// k_cache, v_cache, k_scale, v_scale, slot, k_out, v_out, stream
+PyObject* packed_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    Packed c;
+    int64_t so[3] = {0}, sv[3] = {0};
+    void *k, *v, *stream;
+    int32_t* slot;
+    const int64_t count = size_of(a[4], 1, 0);
+    if (count < 0 || !packed(on, a, false, &c) || !on.in(a[4], at::kInt, {count}, &slot) || !on.here(a[7])) Py_RETURN_NONE;
+    if (c.single) {
+      if (!on.strided(a[5], at::kBFloat16, {count, c.H, c.D}, so + 1, &k, true) || !on.strided(a[6], at::kBFloat16, {count, c.H, c.D}, sv + 1, &v, true))
+        Py_RETURN_NONE;
+    } else if (!on.strided(a[5], at::kBFloat16, {c.L, count, c.H, c.D}, so, &k, true) ||
+               !on.strided(a[6], at::kBFloat16, {c.L, count, c.H, c.D}, sv, &v, true)) {
+      Py_RETURN_NONE;
+    }
+    for (int i = 0; i < 3; ++i)
+      if (so[i] != sv[i]) Py_RETURN_NONE;
+    const spec_rows_t ko = {k, so[0], so[1], so[2]}, vo = {v, sv[0], sv[1], sv[2]};
+    if (!stream_of(a[7], &stream)) return nullptr;
+    return status_of([&] {
+      return f_packed_load(&c.at, c.layer, c.scale_layer, (int32_t)c.L, (int32_t)c.H, (int32_t)c.D, slot, (int32_t)count, &ko, &vo, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
 // addresses of spec_verify, spec_verify_dynamic, spec_advance, spec_tree_metadata, spec_draft; the binding's stream lookup; addresses
-// of spec_tree_attention, spec_cache_extend, spec_cache_store, spec_penalize, spec_verify_tree
+// of spec_tree_attention, spec_cache_extend, spec_cache_store, spec_penalize, spec_verify_tree, spec_rotate_rows, spec_cache_append,
+// spec_packed_append, spec_packed_load
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt;
+  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt, rr, ca, pa, pl;
   PyObject* s;
-  if (!PyArg_ParseTuple(args, "KKKKKOKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt)) return nullptr;
+  if (!PyArg_ParseTuple(args, "KKKKKOKKKKKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt, &rr, &ca, &pa, &pl)) return nullptr;
   f_verify = reinterpret_cast<decltype(f_verify)>(v);
   f_verify_dynamic = reinterpret_cast<decltype(f_verify_dynamic)>(vd);
   f_advance = reinterpret_cast<decltype(f_advance)>(ad);
@@ -465,6 +673,10 @@ PyObject* bind(PyObject*, PyObject* args) {
   f_cache_store = reinterpret_cast<decltype(f_cache_store)>(cs);
   f_penalize = reinterpret_cast<decltype(f_penalize)>(pe);
   f_verify_tree = reinterpret_cast<decltype(f_verify_tree)>(vt);
+  f_rotate_rows = reinterpret_cast<decltype(f_rotate_rows)>(rr);
+  f_cache_append = reinterpret_cast<decltype(f_cache_append)>(ca);
+  f_packed_append = reinterpret_cast<decltype(f_packed_append)>(pa);
+  f_packed_load = reinterpret_cast<decltype(f_packed_load)>(pl);
   for (int i = 0; i < 9; ++i)
     if (!penalty_names[i] && !(penalty_names[i] = PyUnicode_InternFromString(kPenalties[i]))) return nullptr;
   Py_INCREF(s);
@@ -484,6 +696,10 @@ PyMethodDef methods[] = {
     {"cache_store", reinterpret_cast<PyCFunction>(cache_store), METH_FASTCALL, nullptr},
     {"penalize", reinterpret_cast<PyCFunction>(penalize), METH_FASTCALL, nullptr},
     {"verify_tree", reinterpret_cast<PyCFunction>(verify_tree), METH_FASTCALL, nullptr},
+    {"rotate_rows", reinterpret_cast<PyCFunction>(rotate_rows), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(cache_append), METH_FASTCALL, nullptr},
+    {"packed_append", reinterpret_cast<PyCFunction>(packed_append), METH_FASTCALL, nullptr},
+    {"packed_load", reinterpret_cast<PyCFunction>(packed_load), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

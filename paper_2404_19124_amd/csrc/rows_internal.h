@@ -10,6 +10,8 @@ namespace specdraft {
 
 constexpr int64_t kMaxSlots = 1 << 30;   // tokens of a cache, of a block table's row, of a slot map
 
+constexpr int kMaxHeadEntries = 1 << 25;   // rows, or entries, of one call on rows of heads (a launch has fewer than 2^32 threads)
+
 constexpr int kMaxLogitsRows = (1 << 23) - 8;   // rows of one call on logits
 
 // ---- attention of the rows over a paged cache and their own ancestors ----------------
@@ -61,6 +63,61 @@ struct StoreJob {
   int count;
 };
 hipError_t launch_store(const StoreJob& job, hipStream_t st);
+
+// ---- rows of heads: norm, rotation, and into a cache -------------------------------------
+// Rows that one launch reads and writes: the queries and the keys, or the keys and the values.
+struct HeadSide {
+  const uint8_t* from;
+  uint8_t* to;
+  // strides in bytes; far: of sequences, or of layers; to_row: of rows, or of slots
+  int64_t from_far, from_row, from_head, to_far, to_block, to_row, to_head;
+  const float* weight;   // of the norm, or NULL
+  int heads;
+  bool turned;
+};
+struct HeadsJob {
+  HeadSide side[2];
+  int entries, layers, row_words, head_dim;   // 16-byte words of one head's row
+  // rotation: NULL: none; half_words: words of the first elements of the pairs
+  const float *cos, *sin;
+  int n_pos, half_words, pairs;
+  double eps;
+  const int32_t* pos;
+  // rows of trees: entry q * (M + 1) + r
+  int M;
+  const int32_t *ctx_len, *node_depth, *n_nodes;
+  // into a cache: entry t
+  const int32_t *slot, *src_row;
+  int rows, n_slots, block_size;
+  int lanes, trips;      // (the launch's)
+};
+hipError_t launch_heads(HeadsJob job, bool bf16, bool append, hipStream_t st);
+
+// ---- a cache of four bits ------------------------------------------------------------------
+struct PackJob {
+  const uint8_t *k_new, *v_new;
+  uint8_t *k, *v, *k_scale, *v_scale;
+  // strides in bytes
+  int64_t new_layer, new_row, new_head, layer, block, slot_stride, head, scale_layer, scale_block, scale_slot, scale_head;
+  int entries, layers, rows, heads, groups;   // groups of 32 elements of a head
+  const float *cos, *sin, *weight;
+  int n_pos, half_words, pairs;
+  double eps;
+  const int32_t *pos, *slot, *src_row;
+  int n_slots, block_size;
+  int lanes, trips;      // (the launch's)
+};
+hipError_t launch_pack(PackJob job, hipStream_t st);
+
+struct UnpackJob {
+  const uint8_t *k, *v, *k_scale, *v_scale;
+  uint8_t *k_out, *v_out;
+  int64_t layer, block, slot_stride, head, scale_layer, scale_block, scale_slot, scale_head, out_layer, out_row, out_head;
+  int count, layers, heads, groups;
+  const int32_t* slot;
+  int n_slots, block_size;
+};
+hipError_t launch_unpack(const UnpackJob& job, hipStream_t st);
 
 // ---- logits of the rows -------------------------------------------------------------------
 struct LogitsJob {

@@ -176,6 +176,195 @@ extern "C" spec_status_t spec_cache_store(const spec_rows_t* k_new, const spec_r
   return SPEC_OK;
 }
 
+// ---- rows of heads: norm and rotation, into a cache ---------------------------------------------------------------
+
+// Rotation of heads of head_dim elements; pos: whether positions are given
+static spec_status_t check_rotation(const spec_rotation_t* r, int32_t head_dim, int esz, bool pos) {
+  if (!r) return SPEC_OK;
+  if (!r->cos || !r->sin || !pos) return fail(SPEC_EINVAL, "a rotation needs cos, sin and positions");
+  if (r->n_pos < 1) return fail(SPEC_EINVAL, "n_pos must be >= 1");
+  if (r->pairs != 0 && r->pairs != 1) return fail(SPEC_EINVAL, "pairs = %d is neither 0 nor 1", r->pairs);
+  const int per = 32 / esz;   // two words of 16 bytes
+  if (r->rot_dim < per || r->rot_dim > head_dim || r->rot_dim % per)
+    return fail(SPEC_ESHAPE, "rot_dim = %d must be a multiple of %d, at most head_dim = %d", r->rot_dim, per, head_dim);
+  if ((reinterpret_cast<uintptr_t>(r->cos) | reinterpret_cast<uintptr_t>(r->sin)) & 15)
+    return fail(SPEC_EINVAL, "cos and sin must be 16-byte aligned");
+  return SPEC_OK;
+}
+static spec_status_t check_norm(const float* weight, double eps) {
+  if (!weight) return SPEC_OK;
+  if (reinterpret_cast<uintptr_t>(weight) & 15) return fail(SPEC_EINVAL, "weights of a norm must be 16-byte aligned");
+  if (!(eps >= 0) || !(eps < 1e300)) return fail(SPEC_EINVAL, "eps = %g is negative or not finite", eps);
+  return SPEC_OK;
+}
+template <typename Job>
+static void set_rotation(Job& j, const spec_rotation_t* r, int esz) {
+  j.cos = r ? r->cos : nullptr, j.sin = r ? r->sin : nullptr;
+  j.n_pos = r ? r->n_pos : 0, j.half_words = r ? r->rot_dim * esz / 32 : 0, j.pairs = r ? r->pairs : 0;
+}
+
+extern "C" spec_status_t spec_rotate_rows(const spec_rows_t* q, const spec_rows_t* k, const spec_rows_t* q_out, const spec_rows_t* k_out,
+                                          int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                                          const int32_t* pos, const int32_t* ctx_len, const int32_t* node_depth, const int32_t* n_nodes,
+                                          const spec_rotation_t* rotation, const float* q_weight, const float* k_weight, double eps,
+                                          void* hip_stream) {
+  if (!q || !q_out || !q->at || !q_out->at || !k != !k_out || (k && (!k->at || !k_out->at)))
+    return fail(SPEC_EINVAL, "a required pointer is NULL (k and k_out go together)");
+  spec_status_t s = check_heads(dtype, k ? kv_heads : 1, head_dim);
+  if (s != SPEC_OK) return s;
+  if (batch < 1 || M < 0 || q_heads < 1) return fail(SPEC_EINVAL, "batch and q_heads must be >= 1, M >= 0");
+  if (q_heads > 65535 || (k && kv_heads > 65535)) return fail(SPEC_ESHAPE, "q_heads = %d or kv_heads = %d exceeds 65535", q_heads, kv_heads);
+  if ((int64_t)batch * ((int64_t)M + 1) > kMaxHeadEntries) return fail(SPEC_ESHAPE, "batch * (M + 1) exceeds %d", kMaxHeadEntries);
+  if (pos && (ctx_len || node_depth)) return fail(SPEC_EINVAL, "positions are given by pos, or by ctx_len and node_depth");
+  const int esz = element_bytes(dtype);
+  s = check_rotation(rotation, head_dim, esz, pos || (ctx_len && (M == 0 || node_depth)));
+  if (s == SPEC_OK) s = check_norm(q_weight, eps);
+  if (s == SPEC_OK) s = check_norm(k_weight, eps);
+  if (s != SPEC_OK) return s;
+  if (k_weight && !k) return fail(SPEC_EINVAL, "k_weight without k");
+  if (!rows_aligned(*q, esz) || !rows_aligned(*q_out, esz) || (k && (!rows_aligned(*k, esz) || !rows_aligned(*k_out, esz))))
+    return fail(SPEC_EINVAL, "rows of q, k, q_out and k_out must start on multiples of 16 bytes");
+  if (!rows_apart({{batch, q_out->seq_stride}, {M + 1, q_out->row_stride}, {q_heads, q_out->head_stride}}, head_dim) ||
+      (k && !rows_apart({{batch, k_out->seq_stride}, {M + 1, k_out->row_stride}, {kv_heads, k_out->head_stride}}, head_dim)))
+    return fail(SPEC_EINVAL, "rows of q_out or of k_out overlap");
+  HeadsJob j = {};
+  for (int i = 0; i < 2; ++i) {
+    const spec_rows_t *from = i ? k : q, *to = i ? k_out : q_out;
+    if (!from) continue;
+    j.side[i] = {static_cast<const uint8_t*>(from->at), static_cast<uint8_t*>(const_cast<void*>(to->at)), from->seq_stride * esz, from->row_stride * esz,
+                 from->head_stride * esz, to->seq_stride * esz, 0, to->row_stride * esz, to->head_stride * esz, i ? k_weight : q_weight,
+                 i ? kv_heads : q_heads, true};
+  }
+  j.entries = batch * (M + 1), j.layers = 1, j.row_words = head_dim * esz / 16, j.head_dim = head_dim;
+  set_rotation(j, rotation, esz);
+  j.eps = eps, j.pos = pos, j.M = M, j.ctx_len = ctx_len, j.node_depth = node_depth, j.n_nodes = n_nodes;
+  HIP_TRY(launch_heads(j, dtype == SPEC_BF16, false, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
+
+// What spec_cache_append and spec_packed_append check alike; *work: whether there is anything to do
+static spec_status_t check_append(const spec_rows_t* k_new, const spec_rows_t* v_new, int32_t layers, int32_t rows, int32_t kv_heads,
+                                  int32_t head_dim, int32_t dtype, const int32_t* slot, const int32_t* pos, int32_t count,
+                                  const spec_rotation_t* rotation, const float* k_weight, double eps, bool* work) {
+  if (!k_new || !v_new) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  spec_status_t s = check_heads(dtype, kv_heads, head_dim);
+  if (s != SPEC_OK) return s;
+  if (layers < 1 || layers > 65535 || rows < 0 || count < 0)
+    return fail(SPEC_EINVAL, "layers = %d outside [1, 65535], or rows = %d, count = %d negative", layers, rows, count);
+  if (count > kMaxHeadEntries || kv_heads > 65535) return fail(SPEC_ESHAPE, "count = %d exceeds %d, or kv_heads = %d 65535", count, kMaxHeadEntries, kv_heads);
+  const int esz = element_bytes(dtype);
+  *work = count > 0 && rows > 0;
+  if (*work && (!k_new->at || !v_new->at || !slot)) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  s = check_rotation(rotation, head_dim, esz, pos || !*work);
+  if (s == SPEC_OK) s = check_norm(k_weight, eps);
+  if (s != SPEC_OK) return s;
+  if (k_new->seq_stride != v_new->seq_stride || k_new->row_stride != v_new->row_stride || k_new->head_stride != v_new->head_stride)
+    return fail(SPEC_ESHAPE, "k_new and v_new must have the same strides");
+  if (*work && (!rows_aligned(*k_new, esz) || !rows_aligned(*v_new, esz)))
+    return fail(SPEC_EINVAL, "rows of k_new and v_new must start on multiples of 16 bytes");
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_cache_append(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_cache_t* cache,
+                                           int64_t cache_layer_stride, int32_t layers, int32_t rows, int32_t kv_heads, int32_t head_dim,
+                                           int32_t dtype, const int32_t* slot, const int32_t* src_row, const int32_t* pos, int32_t count,
+                                           const spec_rotation_t* rotation, const float* k_weight, double eps, void* hip_stream) {
+  if (!cache) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  bool work = false;
+  spec_status_t s = check_append(k_new, v_new, layers, rows, kv_heads, head_dim, dtype, slot, pos, count, rotation, k_weight, eps, &work);
+  if (s != SPEC_OK) return s;
+  const int esz = element_bytes(dtype);
+  s = check_cache(*cache, esz);
+  if (s != SPEC_OK) return s;
+  if ((uint64_t)(cache_layer_stride * esz) & 15) return fail(SPEC_EINVAL, "rows of the cache must start on multiples of 16 bytes");
+  if (!rows_apart({{layers, cache_layer_stride}, {cache->n_blocks, cache->block_stride}, {cache->block_size, cache->slot_stride}, {kv_heads, cache->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of the cache overlap");
+  if (!work) return SPEC_OK;
+  HeadsJob j = {};
+  for (int i = 0; i < 2; ++i) {
+    const spec_rows_t& from = i ? *v_new : *k_new;
+    j.side[i] = {static_cast<const uint8_t*>(from.at), static_cast<uint8_t*>(const_cast<void*>(i ? cache->v : cache->k)), from.seq_stride * esz,
+                 from.row_stride * esz, from.head_stride * esz, cache_layer_stride * esz, cache->block_stride * esz, cache->slot_stride * esz,
+                 cache->head_stride * esz, i ? nullptr : k_weight, kv_heads, i == 0};
+  }
+  j.entries = count, j.layers = layers, j.row_words = head_dim * esz / 16, j.head_dim = head_dim;
+  set_rotation(j, rotation, esz);
+  j.eps = eps, j.pos = pos, j.slot = slot, j.src_row = src_row, j.rows = rows;
+  j.n_slots = cache->n_blocks * cache->block_size, j.block_size = cache->block_size;
+  HIP_TRY(launch_heads(j, dtype == SPEC_BF16, true, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
+
+// A cache of four bits: rows of head_dim / 2 bytes of codes and head_dim / 32 of scales
+static spec_status_t check_packed(const spec_packed_t* c, int32_t head_dim) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return fail(SPEC_EINVAL, "the cache, or its codes or scales, is NULL");
+  if (head_dim < 32 || head_dim % 32 || head_dim > 256) return fail(SPEC_ESHAPE, "head_dim = %d must be a multiple of 32, at most 256", head_dim);
+  if (c->n_blocks < 1 || c->block_size < 1) return fail(SPEC_EINVAL, "n_blocks and block_size must be >= 1");
+  if ((int64_t)c->n_blocks * c->block_size > kMaxSlots) return fail(SPEC_ESHAPE, "n_blocks * block_size exceeds 2^30");
+  if (!rows_aligned(c->k, c->block_stride, c->slot_stride, c->head_stride, 1) || (reinterpret_cast<uintptr_t>(c->v) & 15))
+    return fail(SPEC_EINVAL, "rows of codes must start on multiples of 16 bytes");
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_packed_append(const spec_rows_t* k_new, const spec_rows_t* v_new, const spec_packed_t* cache,
+                                            int64_t cache_layer_stride, int64_t scale_layer_stride, int32_t layers, int32_t rows,
+                                            int32_t kv_heads, int32_t head_dim, const int32_t* slot, const int32_t* src_row,
+                                            const int32_t* pos, int32_t count, const spec_rotation_t* rotation, const float* k_weight,
+                                            double eps, void* hip_stream) {
+  spec_status_t s = check_packed(cache, head_dim);
+  if (s != SPEC_OK) return s;
+  bool work = false;
+  s = check_append(k_new, v_new, layers, rows, kv_heads, head_dim, SPEC_BF16, slot, pos, count, rotation, k_weight, eps, &work);
+  if (s != SPEC_OK) return s;
+  if (cache_layer_stride & 15) return fail(SPEC_EINVAL, "rows of codes must start on multiples of 16 bytes");
+  if (!rows_apart({{layers, cache_layer_stride}, {cache->n_blocks, cache->block_stride}, {cache->block_size, cache->slot_stride}, {kv_heads, cache->head_stride}}, head_dim / 2) ||
+      !rows_apart({{layers, scale_layer_stride}, {cache->n_blocks, cache->scale_block_stride}, {cache->block_size, cache->scale_slot_stride}, {kv_heads, cache->scale_head_stride}}, head_dim / 32))
+    return fail(SPEC_EINVAL, "rows of the cache overlap");
+  if (!work) return SPEC_OK;
+  PackJob j = {};
+  j.k_new = static_cast<const uint8_t*>(k_new->at), j.v_new = static_cast<const uint8_t*>(v_new->at);
+  j.k = static_cast<uint8_t*>(const_cast<void*>(cache->k)), j.v = static_cast<uint8_t*>(const_cast<void*>(cache->v));
+  j.k_scale = const_cast<uint8_t*>(cache->k_scale), j.v_scale = const_cast<uint8_t*>(cache->v_scale);
+  j.new_layer = k_new->seq_stride * 2, j.new_row = k_new->row_stride * 2, j.new_head = k_new->head_stride * 2;
+  j.layer = cache_layer_stride, j.block = cache->block_stride, j.slot_stride = cache->slot_stride, j.head = cache->head_stride;
+  j.scale_layer = scale_layer_stride, j.scale_block = cache->scale_block_stride, j.scale_slot = cache->scale_slot_stride, j.scale_head = cache->scale_head_stride;
+  j.entries = count, j.layers = layers, j.rows = rows, j.heads = kv_heads, j.groups = head_dim / 32;
+  set_rotation(j, rotation, 2);
+  j.weight = k_weight, j.eps = eps, j.pos = pos, j.slot = slot, j.src_row = src_row;
+  j.n_slots = cache->n_blocks * cache->block_size, j.block_size = cache->block_size;
+  HIP_TRY(launch_pack(j, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_packed_load(const spec_packed_t* cache, int64_t cache_layer_stride, int64_t scale_layer_stride, int32_t layers,
+                                          int32_t kv_heads, int32_t head_dim, const int32_t* slot, int32_t count, const spec_rows_t* k_out,
+                                          const spec_rows_t* v_out, void* hip_stream) {
+  spec_status_t s = check_packed(cache, head_dim);
+  if (s == SPEC_OK) s = check_heads(SPEC_BF16, kv_heads, head_dim);
+  if (s != SPEC_OK) return s;
+  if (!k_out || !v_out) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  if (layers < 1 || layers > 65535 || count < 0) return fail(SPEC_EINVAL, "layers = %d outside [1, 65535], or count = %d negative", layers, count);
+  if (cache_layer_stride & 15) return fail(SPEC_EINVAL, "rows of codes must start on multiples of 16 bytes");
+  if (kv_heads > 65535) return fail(SPEC_ESHAPE, "kv_heads = %d exceeds 65535", kv_heads);
+  if (count == 0) return SPEC_OK;
+  if (!slot || !k_out->at || !v_out->at) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  if (k_out->seq_stride != v_out->seq_stride || k_out->row_stride != v_out->row_stride || k_out->head_stride != v_out->head_stride)
+    return fail(SPEC_ESHAPE, "k_out and v_out must have the same strides");
+  if (!rows_aligned(*k_out, 2) || !rows_aligned(*v_out, 2)) return fail(SPEC_EINVAL, "rows of k_out and v_out must start on multiples of 16 bytes");
+  if (!rows_apart({{layers, k_out->seq_stride}, {count, k_out->row_stride}, {kv_heads, k_out->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of k_out, or of v_out, overlap");
+  UnpackJob j = {};
+  j.k = static_cast<const uint8_t*>(cache->k), j.v = static_cast<const uint8_t*>(cache->v), j.k_scale = cache->k_scale, j.v_scale = cache->v_scale;
+  j.k_out = static_cast<uint8_t*>(const_cast<void*>(k_out->at)), j.v_out = static_cast<uint8_t*>(const_cast<void*>(v_out->at));
+  j.layer = cache_layer_stride, j.block = cache->block_stride, j.slot_stride = cache->slot_stride, j.head = cache->head_stride;
+  j.scale_layer = scale_layer_stride, j.scale_block = cache->scale_block_stride, j.scale_slot = cache->scale_slot_stride, j.scale_head = cache->scale_head_stride;
+  j.out_layer = k_out->seq_stride * 2, j.out_row = k_out->row_stride * 2, j.out_head = k_out->head_stride * 2;
+  j.count = count, j.layers = layers, j.heads = kv_heads, j.groups = head_dim / 32, j.slot = slot;
+  j.n_slots = cache->n_blocks * cache->block_size, j.block_size = cache->block_size;
+  HIP_TRY(launch_unpack(j, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
+
 static spec_status_t check_logits(const void* logits, int32_t dtype, int32_t batch, int32_t M, int32_t vocab,
                                   const spec_penalties_t* pen, const int32_t* node_tok, const int32_t* node_parent) {
   if (!logits) return fail(SPEC_EINVAL, "logits is NULL");

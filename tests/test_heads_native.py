@@ -1,0 +1,85 @@
+"""The native half of the binding for the operators on rows of heads and on a cache of four bits: the usual arguments only, the same
+results as from the checks one by one, and nothing done where an argument is of another kind."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2404_19124_amd import binding as B
+
+
+def calls(dev):
+    """(native name, arguments as the native half takes them, entry point, what it writes)"""
+    g = torch.Generator().manual_seed(11)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    rand = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16).to(dev)
+    byte = lambda *s: torch.randint(100, 140, s, generator=g, dtype=torch.uint8).to(dev)
+    angle = torch.randn((20, 16), generator=g)
+    cos, sin = angle.cos().to(dev), angle.sin().to(dev)
+    weight = lambda *s: torch.rand(s, generator=g).to(dev)
+    got = []
+    for by_pos in (False, True):
+        a = dict(q=rand(2, 3, 4, 64), k=rand(2, 3, 2, 64), q_out=rand(2, 3, 4, 64), k_out=rand(2, 3, 2, 64), cos=cos, sin=sin,
+                 pos=ints([[3, 4, -1], [0, 19, 20]]) if by_pos else None, ctx_len=None if by_pos else ints([5, 9]),
+                 node_depth=None if by_pos else ints([[1, 2], [1, 1]]), n_nodes=None if by_pos else ints([2, 0]),
+                 q_weight=weight(64), k_weight=weight(64), eps=1e-3, pairs=by_pos, stream=None)
+        got.append(("rotate_rows", a, B.spec_rotate_rows, ("q_out", "k_out")))
+    got.append(("rotate_rows", dict(got[0][1], k=None, k_out=None, k_weight=None, q_out=rand(2, 3, 4, 64)), B.spec_rotate_rows, ("q_out",)))
+    for layers in ((), (3,)):
+        a = dict(k_new=rand(*layers, 6, 2, 64), v_new=rand(*layers, 6, 2, 64), slot=ints([9, 17, -1, 2, 30]), k_cache=rand(*layers, 4, 8, 2, 64),
+                 v_cache=rand(*layers, 4, 8, 2, 64), src_row=ints([5, 0, 1, 6, 2]), pos=ints([0, 3, 4, 5, 19]), cos=cos, sin=sin,
+                 k_weight=weight(*layers, 64), eps=1e-3, pairs=True, stream=None)
+        got.append(("cache_append", a, B.spec_cache_append, ("k_cache", "v_cache")))
+        p = dict(k_cache=byte(*layers, 4, 8, 2, 32), v_cache=byte(*layers, 4, 8, 2, 32), k_scale=byte(*layers, 4, 8, 2, 2), v_scale=byte(*layers, 4, 8, 2, 2))
+        a = dict(k_new=a["k_new"], v_new=a["v_new"], slot=a["slot"], **p, **{k: a[k] for k in ("src_row", "pos", "cos", "sin", "k_weight", "eps", "pairs", "stream")})
+        got.append(("packed_append", a, B.spec_packed_append, tuple(p)))
+        a = dict({k: v.clone() for k, v in p.items()}, slot=ints([3, 3, 40, 0]), k_out=rand(*layers, 4, 2, 64), v_out=rand(*layers, 4, 2, 64), stream=None)
+        got.append(("packed_load", a, B.spec_packed_load, ("k_out", "v_out")))
+    return got
+
+
+def test_nothing_happens_on_host_tensors():
+    f = B._native()
+    for name, args, _, wrote in calls("cpu"):
+        before = [args[k].clone() for k in wrote]
+        assert getattr(f, name)(*args.values()) is None
+        assert getattr(f, name)(*list(args.values())[:-1]) is None        # an argument is missing
+        assert getattr(f, name)(*[None] * len(args)) is None
+        assert getattr(f, name)(*["x"] * len(args)) is None
+        assert all(torch.equal(x, args[k]) for x, k in zip(before, wrote))
+
+
+@pytest.mark.gpu
+def test_both_ways_agree_and_the_entry_points_take_the_native_one(monkeypatch):
+    f, taken = B._native(), []
+    fast, slow, through = calls("cuda"), calls("cuda"), calls("cuda")
+    for name, args, _, _ in fast:
+        assert getattr(f, name)(*args.values()) == B.SPEC_OK, name
+    names = {c[0] for c in fast}
+    monkeypatch.setattr(B, "_fast", SimpleNamespace(**{n: lambda *a: None for n in names}))
+    for _, args, call, _ in slow:
+        call(**args)
+    monkeypatch.setattr(B, "_fast", SimpleNamespace(**{n: (lambda n: lambda *a: (taken.append(n), getattr(f, n)(*a))[1])(n) for n in names}))
+    for _, args, call, _ in through:
+        call(**args)
+    assert taken == [c[0] for c in fast]
+    for (name, a, _, wrote), (_, b, _, _), (_, c, _, _) in zip(fast, slow, through):
+        for k in wrote:
+            assert torch.equal(a[k], b[k]) and torch.equal(a[k], c[k]), (name, k)
+
+
+@pytest.mark.gpu
+def test_unusual_arguments_come_back_undone_and_are_refused():
+    f = B._native()
+    for name, call, args in [(n, c, a) for n, a, c, _ in calls("cuda")]:
+        for key, x in args.items():
+            if isinstance(x, torch.Tensor):
+                for bad in (x.cpu(), x.double(), x[:, None], x[..., :1] if x.shape[-1] > 1 else None):
+                    if bad is None or (key == "slot" and bad.dtype == x.dtype and bad.is_cuda and bad.dim() == 1 and args.get("src_row") is None):
+                        continue
+                    assert getattr(f, name)(*dict(args, **{key: bad}).values()) is None, (name, key)
+                    with pytest.raises(ValueError):
+                        call(**dict(args, **{key: bad}))
+        if "eps" in args:
+            assert getattr(f, name)(*dict(args, eps=1).values()) is None
+            assert getattr(f, name)(*dict(args, pairs=1).values()) is None
