@@ -511,6 +511,19 @@ spec_status_t spec_packed_load(const spec_packed_t* cache, int64_t cache_layer_s
                                int32_t kv_heads, int32_t head_dim, const int32_t* slot, int32_t count, const spec_rows_t* k_out,
                                const spec_rows_t* v_out, void* hip_stream);
 
+/* TREE ATTENTION over a cache of four bits: spec_tree_attention in SPEC_BF16 with the values of the codes in the place of the cached keys
+ * and values; everything else, workspace included, is as there.  head_dim is a multiple of 32, at most 256.  A group of scale 255 is not
+ * a number: it reaches the rows that see its token (all of the sequence's), as any such value does. */
+spec_status_t spec_packed_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
+                                    const spec_packed_t* cache, const int32_t* block_table, const int32_t* ctx_len,
+                                    const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out, int32_t batch,
+                                    int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t max_blocks, float scale,
+                                    void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Bytes of workspace such a call needs (host-only). */
+spec_status_t spec_packed_attention_workspace(int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                              int64_t* bytes);
+
 /* Measurement aid, not a step of the method: one launch of a plain copy kernel that
  * reads `bytes` from src (dev) and writes them to dst (dev; must not overlap src).  Its HBM
  * traffic is known exactly, which calibrates the memory-traffic hardware counters that

@@ -23,7 +23,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecdraf
 
 EXPORTS = ["spec_create", "spec_destroy", "spec_draft", "spec_draft_static", "spec_draft_dynamic", "spec_verify", "spec_verify_dynamic", "spec_head_logp", "spec_model_scalars",
            "spec_profile_enable", "spec_profile_read", "spec_copy_probe", "spec_tree_metadata", "spec_advance", "spec_tree_attention", "spec_tree_attention_workspace", "spec_cache_extend",
-           "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_rotate_rows", "spec_cache_append", "spec_packed_append", "spec_packed_load", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
+           "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_rotate_rows", "spec_cache_append", "spec_packed_append", "spec_packed_load",
+           "spec_packed_attention", "spec_packed_attention_workspace", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
 
 
 class SpecError(RuntimeError):
@@ -157,6 +158,10 @@ def lib() -> C.CDLL:
         l.spec_packed_append.argtypes = [rows, rows, packed, C.c_int64, C.c_int64] + [i32] * 4 + [ptr] * 3 + [i32, turn, ptr, dbl, ptr]
         l.spec_packed_load.restype = C.c_int
         l.spec_packed_load.argtypes = [packed, C.c_int64, C.c_int64] + [i32] * 3 + [ptr, i32, rows, rows, ptr]
+        l.spec_packed_attention.restype = C.c_int
+        l.spec_packed_attention.argtypes = [rows] * 3 + [packed] + [ptr] * 4 + [rows] + [i32] * 6 + [C.c_float, ptr, C.c_int64, ptr]
+        l.spec_packed_attention_workspace.restype = C.c_int
+        l.spec_packed_attention_workspace.argtypes = [i32] * 5 + [C.POINTER(C.c_int64)]
         l.spec_copy_probe.restype = C.c_int
         l.spec_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         l.spec_last_error.restype = C.c_char_p
@@ -182,7 +187,7 @@ def _native():
         at = [C.cast(f, C.c_void_p).value for f in (l.spec_verify, l.spec_verify_dynamic, l.spec_advance, l.spec_tree_metadata,
                                                     l.spec_draft, l.spec_tree_attention, l.spec_cache_extend, l.spec_cache_store,
                                                     l.spec_penalize, l.spec_verify_tree, l.spec_rotate_rows, l.spec_cache_append,
-                                                    l.spec_packed_append, l.spec_packed_load)]
+                                                    l.spec_packed_append, l.spec_packed_load, l.spec_packed_attention)]
         _call.bind(*at[:5], lambda stream: _stream_ptr(stream), *at[5:])
         _fast = _call
     return _fast
@@ -1026,6 +1031,55 @@ def spec_packed_load(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torc
     _here(stream, slot=slot, k_out=k_out, v_out=v_out)
     _check(lib().spec_packed_load(C.byref(at), layer, scale_layer, L, KH, D, _ptr(slot), count, C.byref(spec_rows_t(_ptr(k_out), *so)),
                                   C.byref(spec_rows_t(_ptr(v_out), *so)), _stream_ptr(stream)))
+
+
+def spec_packed_attention_workspace(batch: int, R: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    """Bytes of workspace of spec_packed_attention with R rows per sequence (host-only: needs no GPU)."""
+    out = C.c_int64()
+    _check(lib().spec_packed_attention_workspace(int(batch), int(R) - 1, int(q_heads), int(kv_heads), int(head_dim), C.byref(out)))
+    return int(out.value)
+
+
+def spec_packed_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                          k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor, ctx_len: torch.Tensor,
+                          node_parent: Optional[torch.Tensor], n_nodes: Optional[torch.Tensor], out: torch.Tensor,
+                          workspace: torch.Tensor, scale: Optional[float] = None, stream=None) -> None:
+    """Enqueues spec_tree_attention of bfloat16 rows over a cache of four bits.
+
+    Caches as for spec_packed_append (one layer), workspace of spec_packed_attention_workspace() bytes, the others as for
+    spec_tree_attention."""
+    if _CHECK_DEVICE and _done((_fast or _native()).packed_attention(
+            q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, block_table, ctx_len, node_parent, n_nodes, out, workspace, scale, stream)):
+        return
+    if not isinstance(q, torch.Tensor) or q.dim() != 4 or q.dtype != torch.bfloat16:
+        raise ValueError("q must be a bfloat16 tensor [batch, R, q_heads, head_dim]")
+    b, R, H, D = q.shape
+    if R < 1:
+        raise ValueError("q needs a row per sequence")
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a [n_blocks, block_size, kv_heads, head_dim / 2] tensor")
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [batch, max_blocks] tensor")
+    at, _, _, (_, KH, cache_dim) = _packed(*_with_layers(True, k_cache, v_cache, k_scale, v_scale), stream)
+    if cache_dim != D:
+        raise ValueError("q has heads of %d elements, the cache of %d" % (D, cache_dim))
+    sq, so = _strided(q, "q", q.dtype, (b, R, H, D)), _strided(out, "out", q.dtype, (b, R, H, D))
+    sk, sv = _strided(k_new, "k_new", q.dtype, (b, R, KH, D)), _strided(v_new, "v_new", q.dtype, (b, R, KH, D))
+    if sk != sv:
+        raise ValueError("k_new and v_new must have the same strides")
+    _written(out, "out")
+    M, width = R - 1, int(block_table.shape[1])
+    _require(block_table, "block_table", torch.int32, (b, width))
+    _require(ctx_len, "ctx_len", torch.int32, (b,))
+    _require(node_parent, "node_parent", torch.int32, (b, M), optional=M == 0)
+    _require(n_nodes, "n_nodes", torch.int32, (b,), optional=True)
+    _require(workspace, "workspace", torch.uint8)
+    _here(stream, q=q, out=out, k_new=k_new, v_new=v_new, block_table=block_table, ctx_len=ctx_len, node_parent=node_parent, n_nodes=n_nodes,
+          workspace=workspace)
+    _check(lib().spec_packed_attention(
+        C.byref(spec_rows_t(_ptr(q), *sq)), C.byref(spec_rows_t(_ptr(k_new), *sk)), C.byref(spec_rows_t(_ptr(v_new), *sv)), C.byref(at),
+        _ptr(block_table), _ptr(ctx_len), _ptr(node_parent), _ptr(n_nodes), C.byref(spec_rows_t(_ptr(out), *so)), b, M, H, KH, D, width,
+        D ** -0.5 if scale is None else float(scale), _ptr(workspace) or None, workspace.numel(), _stream_ptr(stream)))
 
 
 def spec_plan_contraction(rows: int, k: int, n_head: int, k_top: int, n_proj: int, n_cu: int = 256) -> dict:

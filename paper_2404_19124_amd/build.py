@@ -34,6 +34,7 @@ SOURCES = [
     "kernels_head_once.hip",
     "kernels_tree_meta.hip",
     "kernels_tree_attention.hip",
+    "kernels_packed_attention.hip",
     "kernels_cache.hip",
     "kernels_rows.hip",
     "kernels_heads.hip",

@@ -34,6 +34,7 @@ decltype(&spec_rotate_rows) f_rotate_rows;
 decltype(&spec_cache_append) f_cache_append;
 decltype(&spec_packed_append) f_packed_append;
 decltype(&spec_packed_load) f_packed_load;
+decltype(&spec_packed_attention) f_packed_attention;
 PyObject* f_stream;   // the binding's _stream_ptr
 
 const at::Tensor* tensor(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
@@ -656,13 +657,45 @@ PyObject* packed_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, block_table, ctx_len, node_parent, n_nodes, out, workspace, scale (None or float), stream
+PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 15 || (a[13] != Py_None && !PyFloat_CheckExact(a[13]))) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    Packed c;
+    int64_t d[4], sq[3], so[3], sk[3], sv[3];
+    int32_t code, *table, *ctx, *parent, *count;
+    at::ScalarType dt;
+    void *at[4], *workspace, *stream;
+    if (!floats(a[0], 4, d, &code, &dt) || dt != at::kBFloat16 || d[1] < 1 || !packed(on, a + 3, false, &c) || !c.single || c.D != d[3]) Py_RETURN_NONE;
+    const int64_t width = size_of(a[7], 2, 1), space = tensor(a[12]) ? tensor(a[12])->numel() : -1;
+    if (width < 0 || space < 0 || !on.strided(a[0], dt, {d[0], d[1], d[2], d[3]}, sq, &at[0]) || !on.strided(a[1], dt, {d[0], d[1], c.H, d[3]}, sk, &at[1]) ||
+        !on.strided(a[2], dt, {d[0], d[1], c.H, d[3]}, sv, &at[2]) || !on.in(a[7], at::kInt, {d[0], width}, &table) ||
+        !on.in(a[8], at::kInt, {d[0]}, &ctx) || !on.maybe(a[9], at::kInt, {d[0], d[1] - 1}, &parent) || !on.maybe(a[10], at::kInt, {d[0]}, &count) ||
+        !on.strided(a[11], dt, {d[0], d[1], d[2], d[3]}, so, &at[3], true) || !on.in(a[12], at::kByte, {space}, &workspace) ||
+        (d[1] > 1 && a[9] == Py_None) || !on.here(a[14]))
+      Py_RETURN_NONE;
+    for (int i = 0; i < 3; ++i)
+      if (sk[i] != sv[i]) Py_RETURN_NONE;
+    const spec_rows_t q = {at[0], sq[0], sq[1], sq[2]}, k = {at[1], sk[0], sk[1], sk[2]}, v = {at[2], sv[0], sv[1], sv[2]}, o = {at[3], so[0], so[1], so[2]};
+    const float scale = (float)(a[13] == Py_None ? std::pow((double)d[3], -0.5) : PyFloat_AS_DOUBLE(a[13]));
+    if (!stream_of(a[14], &stream)) return nullptr;
+    return status_of([&] {
+      return f_packed_attention(&q, &k, &v, &c.at, table, ctx, parent, count, &o, (int32_t)d[0], (int32_t)d[1] - 1, (int32_t)d[2], (int32_t)c.H,
+                                (int32_t)d[3], (int32_t)width, scale, workspace, space, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
 // addresses of spec_verify, spec_verify_dynamic, spec_advance, spec_tree_metadata, spec_draft; the binding's stream lookup; addresses
 // of spec_tree_attention, spec_cache_extend, spec_cache_store, spec_penalize, spec_verify_tree, spec_rotate_rows, spec_cache_append,
-// spec_packed_append, spec_packed_load
+// spec_packed_append, spec_packed_load, spec_packed_attention
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt, rr, ca, pa, pl;
+  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt, rr, ca, pa, pl, pt;
   PyObject* s;
-  if (!PyArg_ParseTuple(args, "KKKKKOKKKKKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt, &rr, &ca, &pa, &pl)) return nullptr;
+  if (!PyArg_ParseTuple(args, "KKKKKOKKKKKKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt, &rr, &ca, &pa, &pl, &pt)) return nullptr;
   f_verify = reinterpret_cast<decltype(f_verify)>(v);
   f_verify_dynamic = reinterpret_cast<decltype(f_verify_dynamic)>(vd);
   f_advance = reinterpret_cast<decltype(f_advance)>(ad);
@@ -677,6 +710,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   f_cache_append = reinterpret_cast<decltype(f_cache_append)>(ca);
   f_packed_append = reinterpret_cast<decltype(f_packed_append)>(pa);
   f_packed_load = reinterpret_cast<decltype(f_packed_load)>(pl);
+  f_packed_attention = reinterpret_cast<decltype(f_packed_attention)>(pt);
   for (int i = 0; i < 9; ++i)
     if (!penalty_names[i] && !(penalty_names[i] = PyUnicode_InternFromString(kPenalties[i]))) return nullptr;
   Py_INCREF(s);
@@ -699,6 +733,7 @@ PyMethodDef methods[] = {
     {"rotate_rows", reinterpret_cast<PyCFunction>(rotate_rows), METH_FASTCALL, nullptr},
     {"cache_append", reinterpret_cast<PyCFunction>(cache_append), METH_FASTCALL, nullptr},
     {"packed_append", reinterpret_cast<PyCFunction>(packed_append), METH_FASTCALL, nullptr},
+    {"packed_attention", reinterpret_cast<PyCFunction>(packed_attention), METH_FASTCALL, nullptr},
     {"packed_load", reinterpret_cast<PyCFunction>(packed_load), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -26,11 +26,14 @@ struct AttentionJob {
   int max_blocks, n_blocks, block_size;
   int offsets_fit; // every key lies within 4 GiB of its head's first one, in the cache and among the rows
   int one_place;   // 16 tokens from a multiple of 16 on lie in one block, at offsets of 31 bits
+  const uint8_t *k_scale, *v_scale;               // of a cache of four bits, whose strides above are its codes'
+  int64_t scale_block, scale_slot, scale_head;
   float scale;
   void* workspace;
 };
 int64_t attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim, bool bf16);
 hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st);
+hipError_t launch_packed_attention(const AttentionJob& job, hipStream_t st);   // workspace: attention_workspace's of bfloat16
 
 // ---- block tables and slot maps --------------------------------------------------------
 struct ExtendJob {

@@ -71,22 +71,19 @@ extern "C" spec_status_t spec_tree_attention_workspace(int32_t batch, int32_t M,
   return SPEC_OK;
 }
 
-extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
-                                             const spec_cache_t* cache, const int32_t* block_table, const int32_t* ctx_len,
-                                             const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out,
-                                             int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                                             int32_t dtype, int32_t max_blocks, float scale, void* workspace,
-                                             int64_t workspace_bytes, void* hip_stream) {
-  if (!q || !k_new || !v_new || !cache || !out || !q->at || !k_new->at || !v_new->at || !out->at || !block_table || !ctx_len)
+// What the attentions over a cache of either kind check alike, and what their jobs have in common
+static spec_status_t check_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new, const int32_t* block_table,
+                                     const int32_t* ctx_len, const int32_t* node_parent, const spec_rows_t* out, int32_t batch, int32_t M,
+                                     int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype, int32_t block_size, int32_t max_blocks,
+                                     void* workspace, int64_t workspace_bytes) {
+  if (!q || !k_new || !v_new || !out || !q->at || !k_new->at || !v_new->at || !out->at || !block_table || !ctx_len)
     return fail(SPEC_EINVAL, "a required pointer is NULL");
   spec_status_t s = check_attention_shape(batch, M, q_heads, kv_heads, head_dim, dtype);
   if (s != SPEC_OK) return s;
   if (M > 0 && !node_parent) return fail(SPEC_EINVAL, "node_parent is NULL");
   const int esz = element_bytes(dtype);
-  s = check_cache(*cache, esz);
-  if (s != SPEC_OK) return s;
   if (max_blocks < 1) return fail(SPEC_EINVAL, "max_blocks must be >= 1");
-  if ((int64_t)max_blocks * cache->block_size > kMaxSlots) return fail(SPEC_ESHAPE, "max_blocks * block_size exceeds 2^30");
+  if ((int64_t)max_blocks * block_size > kMaxSlots) return fail(SPEC_ESHAPE, "max_blocks * block_size exceeds 2^30");
   if (k_new->seq_stride != v_new->seq_stride || k_new->row_stride != v_new->row_stride || k_new->head_stride != v_new->head_stride)
     return fail(SPEC_ESHAPE, "k_new and v_new must have the same strides");
   if (!rows_aligned(*q, esz) || !rows_aligned(*k_new, esz) || !rows_aligned(*v_new, esz) || !rows_aligned(*out, esz))
@@ -95,23 +92,48 @@ extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_ro
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SPEC_EINVAL, "workspace of %lld bytes, needed are %lld", (long long)(workspace ? workspace_bytes : 0), (long long)need);
   if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(SPEC_EINVAL, "workspace must be 16-byte aligned");
-  if (!rows_apart({{batch, out->seq_stride}, {M + 1, out->row_stride}, {q_heads, out->head_stride}}, head_dim))
-    return fail(SPEC_EINVAL, "rows of out overlap");
-  AttentionJob j;
-  j.q = q->at, j.k_new = k_new->at, j.v_new = v_new->at, j.k = cache->k, j.v = cache->v, j.out = const_cast<void*>(out->at);
-  j.q_seq = q->seq_stride * esz, j.q_row = q->row_stride * esz, j.q_head = q->head_stride * esz;
-  j.new_seq = k_new->seq_stride * esz, j.new_row = k_new->row_stride * esz, j.new_head = k_new->head_stride * esz;
-  j.out_seq = out->seq_stride * esz, j.out_row = out->row_stride * esz, j.out_head = out->head_stride * esz;
-  j.block = cache->block_stride * esz, j.slot = cache->slot_stride * esz, j.cache_head = cache->head_stride * esz;
+  return SPEC_OK;
+}
+static AttentionJob attention_job(const spec_rows_t& q, const spec_rows_t& k_new, const spec_rows_t& v_new, const spec_rows_t& out,
+                                  const int32_t* block_table, const int32_t* ctx_len, const int32_t* node_parent, const int32_t* n_nodes,
+                                  int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int esz, int32_t max_blocks,
+                                  float scale, void* workspace) {
+  AttentionJob j = {};
+  j.q = q.at, j.k_new = k_new.at, j.v_new = v_new.at, j.out = const_cast<void*>(out.at);
+  j.q_seq = q.seq_stride * esz, j.q_row = q.row_stride * esz, j.q_head = q.head_stride * esz;
+  j.new_seq = k_new.seq_stride * esz, j.new_row = k_new.row_stride * esz, j.new_head = k_new.head_stride * esz;
+  j.out_seq = out.seq_stride * esz, j.out_row = out.row_stride * esz, j.out_head = out.head_stride * esz;
   j.block_table = block_table, j.ctx_len = ctx_len, j.node_parent = node_parent, j.n_nodes = n_nodes;
   j.batch = batch, j.M = M, j.q_heads = q_heads, j.kv_heads = kv_heads, j.head_dim = head_dim;
-  j.max_blocks = max_blocks, j.n_blocks = cache->n_blocks, j.block_size = cache->block_size;
+  j.max_blocks = max_blocks, j.scale = scale, j.workspace = workspace;
+  return j;
+}
+// (strides of 2^31 and more do not multiply beyond 63 bits: a tensor's bytes are addressable)
+static int64_t offsets_most(const AttentionJob& j, int esz) { return (1ll << 32) - 64 - j.head_dim * esz; }
+static bool rows_fit(const AttentionJob& j, int esz) { return j.new_row >= 0 && j.new_row * j.M <= offsets_most(j, esz); }
+
+extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
+                                             const spec_cache_t* cache, const int32_t* block_table, const int32_t* ctx_len,
+                                             const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out,
+                                             int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                             int32_t dtype, int32_t max_blocks, float scale, void* workspace,
+                                             int64_t workspace_bytes, void* hip_stream) {
+  if (!cache) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  spec_status_t s = check_attention(q, k_new, v_new, block_table, ctx_len, node_parent, out, batch, M, q_heads, kv_heads, head_dim, dtype, cache->block_size,
+                                    max_blocks, workspace, workspace_bytes);
+  if (s != SPEC_OK) return s;
+  const int esz = element_bytes(dtype);
+  s = check_cache(*cache, esz);
+  if (s != SPEC_OK) return s;
+  if (!rows_apart({{batch, out->seq_stride}, {M + 1, out->row_stride}, {q_heads, out->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of out overlap");
+  AttentionJob j = attention_job(*q, *k_new, *v_new, *out, block_table, ctx_len, node_parent, n_nodes, batch, M, q_heads, kv_heads, head_dim, esz, max_blocks, scale, workspace);
+  j.k = cache->k, j.v = cache->v;
+  j.block = cache->block_stride * esz, j.slot = cache->slot_stride * esz, j.cache_head = cache->head_stride * esz;
+  j.n_blocks = cache->n_blocks, j.block_size = cache->block_size;
   j.one_place = cache->block_size % 16 == 0 && j.slot >= 0 && j.slot < (1 << 26);
-  // (strides of 2^31 and more do not multiply beyond 63 bits: a tensor's bytes are addressable)
-  const int64_t most = (1ll << 32) - 64 - head_dim * esz;
-  j.offsets_fit = j.block >= 0 && j.slot >= 0 && j.new_row >= 0 && j.new_row * M <= most &&
-                  j.block * (cache->n_blocks - 1) + j.slot * (cache->block_size - 1) <= most;
-  j.scale = scale, j.workspace = workspace;
+  j.offsets_fit = rows_fit(j, esz) && j.block >= 0 && j.slot >= 0 &&
+                  j.block * (cache->n_blocks - 1) + j.slot * (cache->block_size - 1) <= offsets_most(j, esz);
   HIP_TRY(launch_attention(j, dtype == SPEC_BF16, static_cast<hipStream_t>(hip_stream)));
   return SPEC_OK;
 }
@@ -362,6 +384,40 @@ extern "C" spec_status_t spec_packed_load(const spec_packed_t* cache, int64_t ca
   j.count = count, j.layers = layers, j.heads = kv_heads, j.groups = head_dim / 32, j.slot = slot;
   j.n_slots = cache->n_blocks * cache->block_size, j.block_size = cache->block_size;
   HIP_TRY(launch_unpack(j, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_packed_attention_workspace(int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                                         int64_t* bytes) {
+  if (!bytes) return fail(SPEC_EINVAL, "bytes is NULL");
+  spec_status_t s = check_attention_shape(batch, M, q_heads, kv_heads, head_dim, SPEC_BF16);
+  if (s != SPEC_OK) return s;
+  if (head_dim % 32) return fail(SPEC_ESHAPE, "head_dim = %d must be a multiple of 32", head_dim);
+  *bytes = attention_workspace(batch, M, q_heads, kv_heads, head_dim, true);
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_packed_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
+                                               const spec_packed_t* cache, const int32_t* block_table, const int32_t* ctx_len,
+                                               const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out,
+                                               int32_t batch, int32_t M, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                               int32_t max_blocks, float scale, void* workspace, int64_t workspace_bytes,
+                                               void* hip_stream) {
+  spec_status_t s = check_packed(cache, head_dim);
+  if (s != SPEC_OK) return s;
+  s = check_attention(q, k_new, v_new, block_table, ctx_len, node_parent, out, batch, M, q_heads, kv_heads, head_dim, SPEC_BF16, cache->block_size,
+                      max_blocks, workspace, workspace_bytes);
+  if (s != SPEC_OK) return s;
+  if (!rows_apart({{batch, out->seq_stride}, {M + 1, out->row_stride}, {q_heads, out->head_stride}}, head_dim))
+    return fail(SPEC_EINVAL, "rows of out overlap");
+  AttentionJob j = attention_job(*q, *k_new, *v_new, *out, block_table, ctx_len, node_parent, n_nodes, batch, M, q_heads, kv_heads, head_dim, 2, max_blocks, scale, workspace);
+  j.k = cache->k, j.v = cache->v, j.k_scale = cache->k_scale, j.v_scale = cache->v_scale;
+  j.block = cache->block_stride, j.slot = cache->slot_stride, j.cache_head = cache->head_stride;
+  j.scale_block = cache->scale_block_stride, j.scale_slot = cache->scale_slot_stride, j.scale_head = cache->scale_head_stride;
+  j.n_blocks = cache->n_blocks, j.block_size = cache->block_size;
+  j.one_place = cache->block_size % 16 == 0 && j.slot >= 0 && j.slot < (1 << 26) && j.scale_slot >= 0 && j.scale_slot < (1 << 26);
+  j.offsets_fit = rows_fit(j, 2);
+  HIP_TRY(launch_packed_attention(j, static_cast<hipStream_t>(hip_stream)));
   return SPEC_OK;
 }
 

@@ -1,0 +1,271 @@
+"""spec_packed_attention against the 64-bit oracle on the values that its cache's codes stand for, and against spec_tree_attention on
+the same values in bfloat16: the shares, the order of the sums and every rounding are the same, so the bits are."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import heads_oracle as HO
+from paper_2404_19124_amd import binding as B
+from tests.rows_common import dev, exact_float
+from tests.test_gpu_tree_attention import Case, seen_by
+
+pytestmark = pytest.mark.gpu
+
+
+class PackedCase(Case):
+    """Case whose cached keys and values are a cache of four bits; k and v hold what it stands for."""
+
+    def __init__(self, H, KH, D, page, M, ctx, layout="tokens", seed=0, **kw):
+        super().__init__(H, KH, D, page, M, ctx, "bf16", seed=seed, **kw)
+        rng = np.random.default_rng(seed + 1000)
+        shape = self.k.shape[:3] if layout == "tokens" else (self.k.shape[0], KH, page)
+        self.codes, self.scales = [], []
+        for _ in range(2):
+            codes = dev(rng.integers(0, 256, (*shape, D // 2)).astype(np.uint8))
+            scales = dev(rng.integers(124, 128, (*shape, D // 32)).astype(np.uint8))
+            self.codes.append(codes if layout == "tokens" else codes.transpose(1, 2))
+            self.scales.append(scales if layout == "tokens" else scales.transpose(1, 2))
+        self.values()
+
+    def values(self):
+        got = []
+        for codes, scales in zip(self.codes, self.scales):
+            c, s = codes.cpu().numpy(), scales.cpu().numpy()
+            v = np.stack([c & 15, c >> 4], -1).reshape(*c.shape[:-1], -1)
+            v = HO.AMOUNTS[v & 7] * np.where(v & 8, -1.0, 1.0)
+            s = np.where(s == 255, np.nan, 2.0 ** (s.astype(np.float64) - 127))
+            got.append(dev((v * np.repeat(s, 32, -1)).astype(np.float32), torch.bfloat16))
+        self.k, self.v = got
+
+    def packed(self, out=None, **kw):
+        out = torch.full(self.q.shape, 7.0, dtype=self.dtype, device="cuda") if out is None else out
+        n = B.spec_packed_attention_workspace(self.b, self.R, self.H, self.KH, self.D)
+        a = dict(q=self.q, k_new=self.k_new, v_new=self.v_new, k_cache=self.codes[0], v_cache=self.codes[1], k_scale=self.scales[0],
+                 v_scale=self.scales[1], block_table=dev(self.table), ctx_len=dev(self.ctx), node_parent=dev(self.parent),
+                 n_nodes=dev(self.n_nodes), out=out, workspace=torch.full((n,), 255, dtype=torch.uint8, device="cuda"), scale=self.scale)
+        a.update(kw)
+        B.spec_packed_attention(**a)
+        torch.cuda.synchronize()
+        return out
+
+    def check_both(self):
+        got = self.packed()
+        assert torch.equal(got.view(torch.int16), self.run().view(torch.int16))
+        self.check(got)
+        return got
+
+
+CASES = {
+    "chain": dict(H=4, KH=4, D=128, page=16, M=5, ctx=[33, 0, 1, 64, 65]),
+    "one_token": dict(H=8, KH=2, D=64, page=16, M=0, ctx=[0, 1, 63, 64, 500]),
+    "one_sequence": dict(H=2, KH=2, D=128, page=16, M=36, ctx=[300]),
+    "tree_mha": dict(H=3, KH=3, D=128, page=32, M=48, ctx=[0, 17, 128, 255]),
+    "tree_gqa": dict(H=16, KH=2, D=128, page=64, M=40, ctx=[129, 70]),
+    "tree_mqa_odd": dict(H=7, KH=1, D=96, page=7, M=25, ctx=[100, 3, 64]),
+    "wide_tree": dict(H=4, KH=2, D=64, page=16, M=150, ctx=[90, 11]),
+    "pages_of_one": dict(H=2, KH=1, D=64, page=1, M=9, ctx=[70, 2]),
+    "page_over_tile": dict(H=4, KH=4, D=64, page=200, M=12, ctx=[399, 200, 201]),
+    "smallest_head": dict(H=2, KH=2, D=32, page=16, M=12, ctx=[40, 5]),
+    "head_of_160": dict(H=4, KH=1, D=160, page=16, M=12, ctx=[140, 5]),
+    "head_of_192": dict(H=4, KH=1, D=192, page=13, M=12, ctx=[140, 5]),
+    "largest_head": dict(H=2, KH=2, D=256, page=16, M=30, ctx=[140, 5]),
+    "long": dict(H=2, KH=2, D=64, page=16, M=3, ctx=[3000]),
+    "long_grouped": dict(H=8, KH=1, D=128, page=48, M=0, ctx=[5000, 70, 1000]),
+    "long_256": dict(H=32, KH=1, D=256, page=64, M=3, ctx=[1500, 200]),
+    "many_sequences": dict(H=2, KH=1, D=64, page=16, M=6, ctx=[(37 * i) % 90 for i in range(150)]),
+    "loud_scores": dict(H=4, KH=4, D=64, page=16, M=12, ctx=[200, 31], loud=12.0),
+}
+
+
+@pytest.mark.parametrize("layout", ["tokens", "heads"])
+@pytest.mark.parametrize("name", CASES)
+def test_against_the_oracle(name, layout):
+    PackedCase(seed=len(name), layout=layout, **CASES[name]).check_both()
+
+
+def test_shares_that_hold_several_heads():
+    n_nodes = [-1 if q % 11 == 3 else 8 - q % 4 for q in range(128)]
+    PackedCase(H=160, KH=5, D=32, page=16, M=8, ctx=[(37 * q) % 150 for q in range(128)], seed=61, n_nodes=n_nodes).check_both()
+
+
+def test_single_tiles_one_after_the_other():
+    """Units of one tile each, several to a share: with rows of the tree in every one."""
+    PackedCase(H=64, KH=64, D=128, page=16, M=2, ctx=[5, 0, 40, 60, 16, 17] * 10, seed=62).check_both()
+    PackedCase(H=40, KH=40, D=64, page=16, M=0, ctx=[63, 62, 0, 127, 126, 128] * 12, seed=63).check_both()
+
+
+def test_idle_sequences_and_rows_behind_the_last_are_left_as_they_were():
+    c = PackedCase(4, 2, 64, 16, 20, [50, 60, 70, 0, 5], n_nodes=[-1, 0, 20, -1, 7])
+    for q, n in enumerate(c.n_nodes):
+        for t in (c.q, c.k_new, c.v_new):
+            t[q, n + 1:] = float("nan")
+    c.table[0] = -5
+    c.parent[0] = 1 << 20
+    c.check_both()
+
+
+@pytest.mark.parametrize("page", [48, 20])
+def test_slots_past_the_length_may_hold_anything(page):
+    c = PackedCase(4, 2, 128, page, 20, [50, 100, 1, 0], seed=3)
+    for q, n in enumerate(c.ctx):
+        if n % page:
+            c.scales[0][c.table[q, n // page], n % page:] = 255
+            c.scales[1][c.table[q, n // page], n % page:] = 255
+    used = set(int(x) for q, n in enumerate(c.ctx) for x in c.table[q, :-(-n // page)])
+    for x in set(range(c.k.shape[0])) - used:
+        c.scales[0][x], c.scales[1][x] = 255, 255
+    c.values()
+    c.check_both()
+
+
+def test_blocks_out_of_range_take_no_part():
+    c = PackedCase(4, 2, 64, 16, 10, [200, 64, 40], seed=4)
+    c.table[0, 2], c.table[0, 7], c.table[0, 12] = -1, c.k.shape[0], 2 ** 31 - 1
+    c.table[1, :] = -(2 ** 31)     # nothing of the cache is left
+    c.check_both()
+
+
+def test_lengths_and_counts_out_of_range_are_taken_as_the_nearest_within():
+    c = PackedCase(4, 2, 64, 16, 10, [32, 48, 16], seed=5)
+    wild = c.packed(ctx_len=dev(np.array([32, -9, 16], np.int32)), n_nodes=dev(np.array([-7, 10, 1 << 30], np.int32)))
+    c.ctx, c.n_nodes = np.array([32, 0, 16], np.int32), np.array([-1, 10, 10], np.int32)
+    c.check(wild)
+
+
+def test_strides():
+    """Rows out of one product, one layer of a cache with keys and values side by side in a block, an output inside a wider buffer."""
+    c = PackedCase(6, 2, 64, 16, 12, [100, 31, 0], seed=8)
+    fused = torch.full((c.b, c.R, 6 + 2 + 2, 64 + 8), float("nan"), dtype=c.dtype, device="cuda")
+    fused[:, :, :6, :64], fused[:, :, 6:8, :64], fused[:, :, 8:, :64] = c.q, c.k_new, c.v_new
+    n = c.k.shape[0]
+    codes = torch.full((3, n, 2, 2, 16, 48), 0x77, dtype=torch.uint8, device="cuda")
+    scales = torch.full((3, n, 16, 2, 2, 3), 255, dtype=torch.uint8, device="cuda")
+    for i in range(2):
+        codes[1, :, i, :, :, :32] = c.codes[i].transpose(1, 2)
+        scales[1, :, :, i, :, 1:] = c.scales[i]
+    wide = torch.full((c.b, c.R, 6, 3, 64), 7.0, dtype=c.dtype, device="cuda")
+    c.packed(out=wide[:, :, :, 1], q=fused[:, :, :6, :64], k_new=fused[:, :, 6:8, :64], v_new=fused[:, :, 8:, :64],
+             k_cache=codes[1, :, 0, :, :, :32].transpose(1, 2), v_cache=codes[1, :, 1, :, :, :32].transpose(1, 2), k_scale=scales[1, :, :, 0, :, 1:],
+             v_scale=scales[1, :, :, 1, :, 1:])
+    c.check(wide[:, :, :, 1].contiguous())
+    assert (wide[:, :, :, 0] == 7).all() and (wide[:, :, :, 2] == 7).all()
+
+
+def test_out_may_be_q_and_a_negative_scale():
+    c = PackedCase(4, 1, 64, 16, 5, [80, 700], seed=9)
+    c.scale = -0.25
+    want = c.packed()
+    c.check(want)
+    q = c.q.clone()
+    live = dev(np.arange(c.R)[None] <= c.n_nodes[:, None])
+    c.packed(out=q, q=q)
+    assert torch.equal(q[live], want[live])
+
+
+def test_offsets_past_32_bits():
+    """Blocks whose codes lie past 2^32 bytes, and scales past 2^31."""
+    c = PackedCase(2, 1, 64, 16, 6, [40, 33], seed=10)
+    n = c.k.shape[0]
+    for which, stride, row in ((c.codes, (1 << 30) + 32, 32), (c.scales, (1 << 29) + 3, 2)):
+        for i in range(2):
+            big = torch.empty(((n - 1) * stride + 16 * row,), dtype=torch.uint8, device="cuda")
+            view = big.as_strided((n, 16, 1, row), (stride, row, row, 1))
+            view.copy_(which[i])
+            which[i] = view
+    assert (n - 1) * ((1 << 30) + 32) > 1 << 32
+    c.check_both()
+
+
+def test_no_nodes_given():
+    c = PackedCase(4, 2, 64, 16, 0, [100, 0, 7], seed=11)
+    c.check(c.packed(node_parent=None, n_nodes=None))
+    c = PackedCase(4, 2, 64, 16, 9, [100, 0, 7], seed=12, n_nodes=[9, 9, 9])
+    c.check(c.packed(n_nodes=None))
+
+
+def test_another_stream_and_two_at_once():
+    a, b = PackedCase(8, 2, 128, 16, 30, [700, 90, 300], seed=13), PackedCase(8, 2, 128, 16, 30, [500, 400, 0], seed=14)
+    wa, wb = a.packed(), b.packed()
+    outs = [torch.full(x.q.shape, 7.0, dtype=x.dtype, device="cuda") for x in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    spaces = [a.workspace(), b.workspace()]
+    fixed = [dict(block_table=dev(x.table), ctx_len=dev(x.ctx), node_parent=dev(x.parent), n_nodes=dev(x.n_nodes)) for x in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, o, w, f, s in zip((a, b), outs, spaces, fixed, streams):
+            B.spec_packed_attention(x.q, x.k_new, x.v_new, *x.codes, *x.scales, out=o, workspace=w, scale=x.scale, stream=s, **f)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], wa) and torch.equal(outs[1], wb)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    cases = [PackedCase(4, 2, 64, 16, 12, ctx, seed=15 + i) for i, ctx in enumerate(([100, 31, 0], [7, 112, 60], [112, 1, 2]))]
+    live, pool = cases[0], max(c.k.shape[0] for c in cases)
+    width = max(c.table.shape[1] for c in cases)
+    cache = [torch.zeros((pool, *x.shape[1:]), dtype=torch.uint8, device="cuda") for x in (*live.codes, *live.scales)]
+    table = torch.zeros((3, width), dtype=torch.int32, device="cuda")
+    ctx, parent, count = dev(live.ctx), dev(live.parent), dev(live.n_nodes)
+    q, kn, vn, out, space = live.q.clone(), live.k_new.clone(), live.v_new.clone(), torch.zeros_like(live.q), live.workspace()
+
+    def load(c):
+        for to, x in zip(cache, (*c.codes, *c.scales)):
+            to[:x.shape[0]] = x
+        table[:, :c.table.shape[1]] = dev(c.table)
+        for to, x in ((ctx, dev(c.ctx)), (parent, dev(c.parent)), (count, dev(c.n_nodes)), (q, c.q), (kn, c.k_new), (vn, c.v_new)):
+            to.copy_(x)
+        out.fill_(7.0)
+
+    load(live)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        B.spec_packed_attention(q, kn, vn, *cache, table, ctx, parent, count, out, space, live.scale)
+    for c in cases + cases[::-1]:
+        load(c)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out)
+
+
+@pytest.mark.parametrize("H,KH,D,M,ctx", [(2, 2, 64, 9, [5, 0, 40]), (2, 1, 128, 7, [2000, 61]), (8, 2, 128, 20, [300, 3]), (4, 1, 96, 70, [50, 130]),
+                                          (8, 1, 128, 30, [700, 64]), (2, 2, 256, 6, [20, 100]), (4, 2, 192, 60, [90])])
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(H, KH, D, M, ctx):
+    """Infinities and NaN among the nodes' keys and values, as in the attention over 16 bits, to whose bits the result is compared."""
+    c = PackedCase(H, KH, D, 16, M, ctx, seed=21)
+    for row, e, x in ((2, 3, float("inf")), (4, 0, float("nan")), (5, D - 1, float("-inf")), (1, 3, float("-inf"))):
+        c.v_new[:, row, KH - 1, e] = x
+    c.k_new[:, M if M > 6 else 6, 0, 1] = float("nan")
+    got, want = c.packed(), c.run()
+    assert got.isnan().any() and torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.nan_to_num(9.0), want.nan_to_num(9.0))
+    # every row that sees none of them is finite
+    for q in range(c.b):
+        for r in range(c.n_nodes[q] + 1):
+            if not set(seen_by(c.parent[q], r)) & {1, 2, 4, 5, M if M > 6 else 6}:
+                assert got[q, r].isfinite().all()
+
+
+def test_a_group_that_is_not_a_number_reaches_its_sequence_and_head():
+    c = PackedCase(4, 2, 128, 16, 9, [90, 200, 33], seed=22)
+    c.scales[1][c.table[1, 3], 5, 1, 2] = 255       # a value of sequence 1, head 1, elements 64 .. 95
+    c.scales[0][c.table[2, 0], 7, 0, 0] = 255       # a key of sequence 2, head 0
+    got = c.packed()
+    for q in range(3):
+        rows = got[q, :c.n_nodes[q] + 1]
+        bad = rows.isnan()
+        want = torch.zeros_like(bad)
+        if q == 1:
+            want[:, 2:, 64:96] = True
+        if q == 2:
+            want[:, :2] = True
+        assert torch.equal(bad, want), q
+        assert rows[~want].isfinite().all()
+
+
+def test_values_that_are_all_the_same_come_out_as_they_are():
+    c = PackedCase(8, 2, 128, 16, 12, [300, 2, 0], seed=23)
+    c.codes[1][:], c.scales[1][:], c.v_new[:] = 0x55, 120, 3 * 2.0 ** -7
+    got = c.packed()
+    for q in range(3):
+        assert (got[q, :c.n_nodes[q] + 1] == 3 * 2.0 ** -7).all()

@@ -35,6 +35,12 @@ def calls(dev):
         got.append(("packed_append", a, B.spec_packed_append, tuple(p)))
         a = dict({k: v.clone() for k, v in p.items()}, slot=ints([3, 3, 40, 0]), k_out=rand(*layers, 4, 2, 64), v_out=rand(*layers, 4, 2, 64), stream=None)
         got.append(("packed_load", a, B.spec_packed_load, ("k_out", "v_out")))
+    p = dict(k_cache=byte(6, 8, 2, 32), v_cache=byte(6, 8, 2, 32), k_scale=byte(6, 8, 2, 2), v_scale=byte(6, 8, 2, 2))
+    space = torch.empty(B.spec_packed_attention_workspace(2, 4, 4, 2, 64), dtype=torch.uint8, device=dev)
+    for scale in (None, 0.3):
+        a = dict(q=rand(2, 4, 4, 64), k_new=rand(2, 4, 2, 64), v_new=rand(2, 4, 2, 64), **p, block_table=ints([[0, 3], [5, 1]]), ctx_len=ints([11, 3]),
+                 node_parent=ints([[-1, 0, 0], [-1, -1, 1]]), n_nodes=ints([3, 3]), out=rand(2, 4, 4, 64), workspace=space, scale=scale, stream=None)
+        got.append(("packed_attention", a, B.spec_packed_attention, ("out",)))
     return got
 
 
@@ -75,6 +81,8 @@ def test_unusual_arguments_come_back_undone_and_are_refused():
         for key, x in args.items():
             if isinstance(x, torch.Tensor):
                 for bad in (x.cpu(), x.double(), x[:, None], x[..., :1] if x.shape[-1] > 1 else None):
+                    if bad is not None and key == "workspace" and bad.dtype == x.dtype and bad.is_cuda:
+                        continue   # (one of any shape)
                     if bad is None or (key == "slot" and bad.dtype == x.dtype and bad.is_cuda and bad.dim() == 1 and args.get("src_row") is None):
                         continue
                     assert getattr(f, name)(*dict(args, **{key: bad}).values()) is None, (name, key)

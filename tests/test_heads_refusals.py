@@ -112,6 +112,31 @@ def test_packed_load(kw, status):
     assert B.spec_last_error()
 
 
+def attention(**kw):
+    a = dict(q=rows(), k_new=rows(), v_new=rows(), cache=packed(), block_table=P, ctx_len=P, node_parent=P, n_nodes=P, out=rows(), batch=2, M=4, q_heads=4,
+             kv_heads=2, head_dim=64, max_blocks=3, scale=1.0, workspace=P, bytes=1 << 40, stream=None)
+    return call("spec_packed_attention", dict(a, **kw))
+
+
+@pytest.mark.parametrize("kw,status", PACKED + [
+    (dict(cache=None), B.SPEC_EINVAL), (dict(q=None), B.SPEC_EINVAL), (dict(out=rows(at=None)), B.SPEC_EINVAL), (dict(block_table=None), B.SPEC_EINVAL),
+    (dict(ctx_len=None), B.SPEC_EINVAL), (dict(node_parent=None), B.SPEC_EINVAL), (dict(batch=0), B.SPEC_EINVAL), (dict(M=4097), B.SPEC_ESHAPE),
+    (dict(q_heads=5), B.SPEC_ESHAPE), (dict(head_dim=288), B.SPEC_ESHAPE), (dict(max_blocks=0), B.SPEC_EINVAL), (dict(max_blocks=1 << 27), B.SPEC_ESHAPE),
+    (dict(v_new=rows(seq=1 << 13)), B.SPEC_ESHAPE), (dict(q=rows(at=P + 8)), B.SPEC_EINVAL), (dict(workspace=None), B.SPEC_EINVAL), (dict(bytes=100), B.SPEC_EINVAL),
+    (dict(workspace=P + 4), B.SPEC_EINVAL), (dict(out=rows(row=64)), B.SPEC_EINVAL)])
+def test_packed_attention(kw, status):
+    assert attention(**kw) == status, B.spec_last_error()
+    assert B.spec_last_error()
+
+
+def test_packed_attention_workspace():
+    assert B.spec_packed_attention_workspace(2, 5, 4, 2, 64) == B.spec_tree_attention_workspace(2, 5, 4, 2, 64, torch.bfloat16)
+    for bad in ((0, 5, 4, 2, 64), (2, 5, 4, 3, 64), (2, 5, 4, 2, 48), (2, 0, 4, 2, 64)):
+        with pytest.raises(B.SpecError):
+            B.spec_packed_attention_workspace(*bad)
+    assert B.lib().spec_packed_attention_workspace(2, 4, 4, 2, 64, None) == B.SPEC_EINVAL
+
+
 def test_the_binding_checks_tensors(monkeypatch):
     monkeypatch.setattr(B, "_CHECK_DEVICE", False)
     bf, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
@@ -170,3 +195,19 @@ def test_the_binding_checks_tensors(monkeypatch):
     pack("must not be expanded", k_cache=z(1, 8, 2, 32, t=u8).expand(4, 8, 2, 32), v_cache=z(1, 8, 2, 32, t=u8).expand(4, 8, 2, 32))
     pack("k_out must have shape", True, k_out=z(6, 2, 64))
     pack("same strides", True, v_out=z(2, 7, 64).transpose(0, 1))
+
+    def att(match, **kw):
+        a = dict(q=z(2, 3, 4, 64), k_new=z(2, 3, 2, 64), v_new=z(2, 3, 2, 64), k_cache=z(4, 8, 2, 32, t=u8), v_cache=z(4, 8, 2, 32, t=u8), k_scale=z(4, 8, 2, 2, t=u8),
+                 v_scale=z(4, 8, 2, 2, t=u8), block_table=z(2, 5, t=i32), ctx_len=z(2, t=i32), node_parent=z(2, 2, t=i32), n_nodes=z(2, t=i32),
+                 out=z(2, 3, 4, 64), workspace=z(9, t=u8), stream=STREAM)
+        with pytest.raises(ValueError, match=match):
+            B.spec_packed_attention(**dict(a, **kw))
+
+    att("q must be a bfloat16", q=z(2, 3, 4, 64, t=torch.float32))
+    att("k_cache must be", k_cache=z(1, 4, 8, 2, 32, t=u8))
+    att("heads of 64 elements, the cache of 32", **{k: z(4, 8, 2, n, t=u8) for k, n in (("k_cache", 16), ("v_cache", 16), ("k_scale", 1), ("v_scale", 1))})
+    att("k_new must have shape", k_new=z(2, 3, 1, 64))
+    att("must not be expanded", out=z(2, 1, 4, 64).expand(2, 3, 4, 64))
+    att("block_table must be", block_table=z(5, t=i32))
+    att("node_parent is required", node_parent=None)
+    att("workspace must have dtype", workspace=z(9, t=i32))
