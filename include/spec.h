@@ -438,6 +438,37 @@ spec_status_t spec_verify_tree(const void* logits, int32_t logits_dtype, const i
                                int32_t* out_tokens, int32_t* n_out, int32_t* path_row, int32_t* accept_all,
                                int32_t* counts_out, uint32_t* seen_out, void* hip_stream);
 
+/* VERIFY against the base model's probabilities (Sec. 1: speculative decoding keeps the base model's distribution), on the rows of the
+ * tree, from given random numbers, with the penalties applied on the fly.  With v the processed logits of a row as spec_penalize gives
+ * them in float32 (NaN taken as -inf), T = temperature[q] > 0 and, in 64 bits, w_t = exp((v_t - max v) / T) (where max v is infinite:
+ * 1 for the infinite ones, 0 for others) and S their sum:
+ *     the row's mass S is laid out as the row's nodes' tokens in the order of their nodes (of siblings with the same token the first one,
+ *     no token outside [0, vocab)), then all other tokens by number; its token is the one in whose stretch u * S lies, u =
+ *     uniform[q][depth of the row] (taken as the nearest within [0, 1));
+ *     where that is a node's token the path goes down to the node, else it ends.  At depth n_predict a row's nodes are not looked at.
+ * Started at row 0, the path's tokens are emitted.  So the tokens are distributed as without speculation, for uniform random numbers.
+ * T <= 0 or NaN: the first maximum has all of the mass.  A row with nothing above -inf: token 0.
+ *   logits      dev [batch, R, vocab] logits_dtype;  pen host, may be NULL (rows then do not count their paths)
+ *   node_tok, node_parent [batch, M], n_nodes [batch]: as for spec_tree_attention and spec_penalize; required if M > 0 (n_nodes NULL: M)
+ *   temperature dev [batch] float32, NULL: 1;  uniform dev [batch, n_predict + 1] float32
+ * Outputs (dev, int32 but for out_logp):
+ *   accept_len, n_out = accept_len + 1 [batch], out_tokens, path_row [batch, n_predict + 1]: as spec_verify_tree's
+ *   out_logp    [batch, n_predict + 1] float32, may be NULL: logarithm of the emitted tokens' w / S (0 without a temperature, -inf in a
+ *               row with nothing above -inf); 0 behind the last one
+ *   counts_out, seen_out                 as for spec_verify_tree
+ *   workspace   dev, 16-byte aligned, at least spec_verify_sampled_workspace() bytes, contents of no meaning before and after;
+ *               calls that may overlap in time, replays of graphs among them, need one each
+ * The same call gives the same bits.  M <= 4096, 0 <= n_predict <= SPEC_MAX_STAGES, batch * R <= 2^20, batch <= 2^17, vocab <= 2^30. */
+spec_status_t spec_verify_sampled(const void* logits, int32_t logits_dtype, const int32_t* node_tok, const int32_t* node_parent,
+                                  const int32_t* n_nodes, const spec_penalties_t* pen, const float* temperature,
+                                  const float* uniform, int32_t batch, int32_t M, int32_t n_predict, int32_t vocab,
+                                  int32_t* accept_len, int32_t* out_tokens, int32_t* n_out, int32_t* path_row, float* out_logp,
+                                  int32_t* counts_out, uint32_t* seen_out, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream);
+
+/* Bytes of workspace such a call needs (host-only). */
+spec_status_t spec_verify_sampled_workspace(int32_t batch, int32_t M, int32_t vocab, int32_t logits_dtype, int64_t* bytes);
+
 /* ---- rotation and norms of heads, and a cache of four bits ----------------------------------------------------
  * Table of a rotation: the pair i of a head (i < rot_dim / 2) at position x is turned by the angle whose cosine and sine are
  * cos[x][i] and sin[x][i]:  (a, b) -> (a cos - b sin, b cos + a sin).  The pair is the elements i and i + rot_dim / 2, or with

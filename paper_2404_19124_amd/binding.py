@@ -24,7 +24,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecdraf
 EXPORTS = ["spec_create", "spec_destroy", "spec_draft", "spec_draft_static", "spec_draft_dynamic", "spec_verify", "spec_verify_dynamic", "spec_head_logp", "spec_model_scalars",
            "spec_profile_enable", "spec_profile_read", "spec_copy_probe", "spec_tree_metadata", "spec_advance", "spec_tree_attention", "spec_tree_attention_workspace", "spec_cache_extend",
            "spec_cache_store", "spec_penalize", "spec_verify_tree", "spec_rotate_rows", "spec_cache_append", "spec_packed_append", "spec_packed_load",
-           "spec_packed_attention", "spec_packed_attention_workspace", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
+           "spec_packed_attention", "spec_packed_attention_workspace", "spec_verify_sampled", "spec_verify_sampled_workspace", "spec_plan_contraction", "spec_plan_head", "spec_plan_panel", "spec_last_error", "spec_version"]
 
 
 class SpecError(RuntimeError):
@@ -162,6 +162,10 @@ def lib() -> C.CDLL:
         l.spec_packed_attention.argtypes = [rows] * 3 + [packed] + [ptr] * 4 + [rows] + [i32] * 6 + [C.c_float, ptr, C.c_int64, ptr]
         l.spec_packed_attention_workspace.restype = C.c_int
         l.spec_packed_attention_workspace.argtypes = [i32] * 5 + [C.POINTER(C.c_int64)]
+        l.spec_verify_sampled.restype = C.c_int
+        l.spec_verify_sampled.argtypes = [ptr, i32, ptr, ptr, ptr, pen, ptr, ptr] + [i32] * 4 + [ptr] * 8 + [C.c_int64, ptr]
+        l.spec_verify_sampled_workspace.restype = C.c_int
+        l.spec_verify_sampled_workspace.argtypes = [i32] * 4 + [C.POINTER(C.c_int64)]
         l.spec_copy_probe.restype = C.c_int
         l.spec_copy_probe.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         l.spec_last_error.restype = C.c_char_p
@@ -187,7 +191,8 @@ def _native():
         at = [C.cast(f, C.c_void_p).value for f in (l.spec_verify, l.spec_verify_dynamic, l.spec_advance, l.spec_tree_metadata,
                                                     l.spec_draft, l.spec_tree_attention, l.spec_cache_extend, l.spec_cache_store,
                                                     l.spec_penalize, l.spec_verify_tree, l.spec_rotate_rows, l.spec_cache_append,
-                                                    l.spec_packed_append, l.spec_packed_load, l.spec_packed_attention)]
+                                                    l.spec_packed_append, l.spec_packed_load, l.spec_packed_attention,
+                                                    l.spec_verify_sampled)]
         _call.bind(*at[:5], lambda stream: _stream_ptr(stream), *at[5:])
         _fast = _call
     return _fast
@@ -841,6 +846,60 @@ def spec_verify_tree(logits: torch.Tensor, cand_tokens: torch.Tensor, cand_node:
         _ptr(node_parent) or None, _ptr(n_nodes), C.byref(pen) if pen is not None else None, b, R - 1, Bc, n, V, _ptr(greedy),
         _ptr(accept_len), _ptr(best_cand), _ptr(out_tokens), _ptr(n_out), _ptr(path_row), _ptr(accept_all),
         pen.counts if update else None, pen.seen if update else None, _stream_ptr(stream)))
+
+
+def spec_verify_sampled_workspace(batch: int, R: int, vocab: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace of spec_verify_sampled on logits [batch, R, vocab] (host-only: needs no GPU)."""
+    out = C.c_int64()
+    _check(lib().spec_verify_sampled_workspace(int(batch), int(R) - 1, int(vocab), _DTYPE_CODE.get(dtype, -1), C.byref(out)))
+    return int(out.value)
+
+
+def spec_verify_sampled(logits: torch.Tensor, uniform: torch.Tensor, n_nodes: Optional[torch.Tensor], accept_len: torch.Tensor,
+                        out_tokens: torch.Tensor, n_out: torch.Tensor, path_row: torch.Tensor, workspace: torch.Tensor,
+                        out_logp: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                        penalties: Optional[Dict[str, torch.Tensor]] = None, node_tok: Optional[torch.Tensor] = None,
+                        node_parent: Optional[torch.Tensor] = None, update: bool = False, stream=None) -> None:
+    """Enqueues one verify of the tree's nodes against the probabilities of logits [batch, R, vocab], from given random numbers.
+
+    uniform [batch, n + 1] float32 in [0, 1), one per depth; temperature [batch] float32 (None: 1; 0: the first maximum); node_tok,
+    node_parent [batch, R - 1] (required if R > 1); accept_len, n_out [batch]; out_tokens, path_row [batch, n + 1]; out_logp
+    [batch, n + 1] float32: the emitted tokens' logarithms of probability.  penalties, update: as for spec_verify_tree.  workspace:
+    contiguous uint8, spec_verify_sampled_workspace() bytes, not shared by calls that may overlap in time."""
+    if _CHECK_DEVICE and _done((_fast or _native()).verify_sampled(
+            logits, uniform, n_nodes, accept_len, out_tokens, n_out, path_row, workspace, out_logp, temperature, penalties, node_tok,
+            node_parent, update, stream)):
+        return
+    code = _float_code(logits, "logits", (3,))
+    b, R, V = logits.shape
+    if R < 1:
+        raise ValueError("logits need a row per sequence")
+    if not isinstance(uniform, torch.Tensor) or uniform.dim() != 2 or uniform.shape[1] < 1:
+        raise ValueError("uniform must be a [batch, n_predict + 1] tensor")
+    n1, i32, f32 = int(uniform.shape[1]), torch.int32, torch.float32
+    _require(logits, "logits", logits.dtype)
+    _require(uniform, "uniform", f32, (b, n1))
+    for t, name in ((accept_len, "accept_len"), (n_out, "n_out")):
+        _require(t, name, i32, (b,))
+    for t, name in ((out_tokens, "out_tokens"), (path_row, "path_row")):
+        _require(t, name, i32, (b, n1))
+    _require(out_logp, "out_logp", f32, (b, n1), optional=True)
+    _require(temperature, "temperature", f32, (b,), optional=True)
+    _require(n_nodes, "n_nodes", i32, (b,), optional=True)
+    for t, name in ((node_tok, "node_tok"), (node_parent, "node_parent")):
+        _require(t, name, i32, (b, R - 1), optional=R == 1)
+    if (node_tok is None) != (node_parent is None):
+        raise ValueError("node_tok and node_parent go together")
+    _require(workspace, "workspace", torch.uint8)
+    pen = None if penalties is None else _penalties(penalties, b, R, V, stream)
+    if update and pen is None:
+        raise ValueError("update needs penalties")
+    _here(stream, logits=logits, uniform=uniform, n_nodes=n_nodes, accept_len=accept_len, out_tokens=out_tokens, n_out=n_out, path_row=path_row,
+          workspace=workspace, out_logp=out_logp, temperature=temperature, node_tok=node_tok, node_parent=node_parent)
+    _check(lib().spec_verify_sampled(
+        _ptr(logits), code, _ptr(node_tok) or None, _ptr(node_parent) or None, _ptr(n_nodes), _by(pen), _ptr(temperature), _ptr(uniform), b, R - 1,
+        n1 - 1, V, _ptr(accept_len), _ptr(out_tokens), _ptr(n_out), _ptr(path_row), _ptr(out_logp), pen.counts if update else None,
+        pen.seen if update else None, _ptr(workspace) or None, workspace.numel(), _stream_ptr(stream)))
 
 
 # ---- rotation and norms of heads, and a cache of four bits ----

@@ -37,6 +37,7 @@ SOURCES = [
     "kernels_packed_attention.hip",
     "kernels_cache.hip",
     "kernels_rows.hip",
+    "kernels_sample.hip",
     "kernels_heads.hip",
     "rows_lib.hip",
 ]

@@ -35,6 +35,7 @@ decltype(&spec_cache_append) f_cache_append;
 decltype(&spec_packed_append) f_packed_append;
 decltype(&spec_packed_load) f_packed_load;
 decltype(&spec_packed_attention) f_packed_attention;
+decltype(&spec_verify_sampled) f_verify_sampled;
 PyObject* f_stream;   // the binding's _stream_ptr
 
 const at::Tensor* tensor(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
@@ -454,6 +455,39 @@ PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// logits, uniform, n_nodes, accept_len, out_tokens, n_out, path_row, workspace, out_logp, temperature, penalties, node_tok, node_parent,
+// update, stream
+PyObject* verify_sampled(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 15 || (a[11] == Py_None) != (a[12] == Py_None) || !PyBool_Check(a[13]) || (a[13] == Py_True && a[10] == Py_None)) Py_RETURN_NONE;
+  try {
+    const Rows on;
+    int64_t d[3];
+    int32_t code, *count, *len, *out, *n_out, *path, *tok, *parent;
+    float *uniform, *logp, *temperature;
+    at::ScalarType dt;
+    void *logits, *workspace, *stream;
+    spec_penalties_t pen = {};
+    const int64_t n1 = size_of(a[1], 2, 1), space = tensor(a[7]) ? tensor(a[7])->numel() : -1;
+    if (n1 < 1 || space < 0 || !floats(a[0], 3, d, &code, &dt) || d[1] < 1 || !on.in(a[0], dt, {d[0], d[1], d[2]}, &logits)) Py_RETURN_NONE;
+    const int64_t b = d[0], R = d[1];
+    if ((R > 1 && a[11] == Py_None) || !on.in(a[1], at::kFloat, {b, n1}, &uniform) || !on.maybe(a[2], at::kInt, {b}, &count) ||
+        !on.in(a[3], at::kInt, {b}, &len) || !on.in(a[4], at::kInt, {b, n1}, &out) || !on.in(a[5], at::kInt, {b}, &n_out) ||
+        !on.in(a[6], at::kInt, {b, n1}, &path) || !on.in(a[7], at::kByte, {space}, &workspace) || !on.maybe(a[8], at::kFloat, {b, n1}, &logp) ||
+        !on.maybe(a[9], at::kFloat, {b}, &temperature) || (a[10] != Py_None && !penalties(on, a[10], b, R, d[2], &pen)) ||
+        !on.maybe(a[11], at::kInt, {b, R - 1}, &tok) || !on.maybe(a[12], at::kInt, {b, R - 1}, &parent) || !on.here(a[14]))
+      Py_RETURN_NONE;
+    const bool update = a[13] == Py_True;
+    if (!stream_of(a[14], &stream)) return nullptr;
+    return status_of([&] {
+      return f_verify_sampled(logits, code, tok, parent, count, a[10] == Py_None ? nullptr : &pen, temperature, uniform, (int32_t)b, (int32_t)R - 1,
+                              (int32_t)n1 - 1, (int32_t)d[2], len, out, n_out, path, logp, update ? const_cast<int32_t*>(pen.counts) : nullptr,
+                              update ? const_cast<uint32_t*>(pen.seen) : nullptr, workspace, space, stream);
+    });
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
 // cos, sin (both None: no rotation), pairs; false: not the usual case
 struct Turn {
   spec_rotation_t r;
@@ -691,11 +725,11 @@ PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // addresses of spec_verify, spec_verify_dynamic, spec_advance, spec_tree_metadata, spec_draft; the binding's stream lookup; addresses
 // of spec_tree_attention, spec_cache_extend, spec_cache_store, spec_penalize, spec_verify_tree, spec_rotate_rows, spec_cache_append,
-// spec_packed_append, spec_packed_load, spec_packed_attention
+// spec_packed_append, spec_packed_load, spec_packed_attention, spec_verify_sampled
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt, rr, ca, pa, pl, pt;
+  unsigned long long v, vd, ad, tm, dr, ta, ce, cs, pe, vt, rr, ca, pa, pl, pt, vs;
   PyObject* s;
-  if (!PyArg_ParseTuple(args, "KKKKKOKKKKKKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt, &rr, &ca, &pa, &pl, &pt)) return nullptr;
+  if (!PyArg_ParseTuple(args, "KKKKKOKKKKKKKKKKK", &v, &vd, &ad, &tm, &dr, &s, &ta, &ce, &cs, &pe, &vt, &rr, &ca, &pa, &pl, &pt, &vs)) return nullptr;
   f_verify = reinterpret_cast<decltype(f_verify)>(v);
   f_verify_dynamic = reinterpret_cast<decltype(f_verify_dynamic)>(vd);
   f_advance = reinterpret_cast<decltype(f_advance)>(ad);
@@ -711,6 +745,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   f_packed_append = reinterpret_cast<decltype(f_packed_append)>(pa);
   f_packed_load = reinterpret_cast<decltype(f_packed_load)>(pl);
   f_packed_attention = reinterpret_cast<decltype(f_packed_attention)>(pt);
+  f_verify_sampled = reinterpret_cast<decltype(f_verify_sampled)>(vs);
   for (int i = 0; i < 9; ++i)
     if (!penalty_names[i] && !(penalty_names[i] = PyUnicode_InternFromString(kPenalties[i]))) return nullptr;
   Py_INCREF(s);
@@ -733,6 +768,7 @@ PyMethodDef methods[] = {
     {"rotate_rows", reinterpret_cast<PyCFunction>(rotate_rows), METH_FASTCALL, nullptr},
     {"cache_append", reinterpret_cast<PyCFunction>(cache_append), METH_FASTCALL, nullptr},
     {"packed_append", reinterpret_cast<PyCFunction>(packed_append), METH_FASTCALL, nullptr},
+    {"verify_sampled", reinterpret_cast<PyCFunction>(verify_sampled), METH_FASTCALL, nullptr},
     {"packed_attention", reinterpret_cast<PyCFunction>(packed_attention), METH_FASTCALL, nullptr},
     {"packed_load", reinterpret_cast<PyCFunction>(packed_load), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "device_utils.h"
+#include "row_penalty.h"
 #include "rows_internal.h"
 #include "spec_internal.h"
 
@@ -16,37 +17,6 @@ constexpr int row_chunks(bool out) { return out ? 1 : 2; }   // chunks of 8 toke
 // and 16.4 us, 256 rows 19.3 and 22.3; from 280 to 500, where two rows share a CU (bfloat16) or take turns (float32: 120 KiB of LDS
 // each), 25.9 to 30.2 and 26.4 to 29.3, alike; 650 bfloat16 rows 32.4 and 25.4, float32 38.2 and 40.5.
 constexpr int kWideRows = 512;
-
-// eight neighbours; rows of an odd length start anywhere, so their words are not aligned to 16 bytes (the compiler's memcpy is one
-// 16-byte load all the same)
-template <typename T>
-__device__ __forceinline__ T load_words(const void* from) {
-  T x;
-  __builtin_memcpy(&x, from, sizeof(T));
-  return x;
-}
-
-__device__ __forceinline__ float to_f32(uint16_t x) { return bf16_bits_to_f32(x); }
-__device__ __forceinline__ float to_f32(float x) { return x; }
-
-// What changes one sequence's logits (row by row: allowed).
-struct RowPenalty {
-  const int32_t* counts;
-  const uint32_t *seen, *allowed;
-  const float* bias;
-  float rep, pres, freq;
-};
-
-// A token by the whole formula; c: its occurrences.
-__device__ __forceinline__ float penalized(float v, int c, bool bit, float bias, bool allowed, const RowPenalty& pen) {
-// (a product and a difference are rounded one by one: what is chosen must not hang on the compiler's choice)
-#pragma clang fp contract(off)
-  if (bit || c > 0) v = v > 0.0f ? v / pen.rep : v * pen.rep;
-  v = v - pen.freq * (float)c;
-  if (c > 0) v = v - pen.pres;
-  if (pen.bias) v = v + bias;
-  return allowed ? v : SPEC_NEG_INF;
-}
 
 // One workgroup per row, or (OUT, few rows) per `span` tokens of a row.  Few tokens of a row were seen or are on its path: TOUCHED
 // tokens, and with them the last V % 8.  The others only take a bias and a mask, eight at a time, all loads of a trip requested a
@@ -90,15 +60,7 @@ __global__ __launch_bounds__(NT, 4) void logits_kernel(LogitsJob p, int span) {
   const T* row = static_cast<const T*>(p.logits) + (int64_t)me * V;
   T* out = OUT ? static_cast<T*>(p.out) + (int64_t)me * V : nullptr;
   const int begin = OUT ? (int)blockIdx.y * span : 0, end = OUT ? min(V, begin + span) : V, full = end & ~7;
-  const int n_words = (V + 31) / 32;
-  RowPenalty pen;
-  pen.counts = p.pen.counts ? p.pen.counts + (int64_t)q * V : nullptr;
-  pen.seen = p.pen.seen ? p.pen.seen + (int64_t)q * n_words : nullptr;
-  const int mask_row = p.pen.allowed ? p.pen.mask_row[me] : -1, bias_row = p.pen.bias ? p.pen.bias_row[q] : -1;
-  pen.bias = bias_row >= 0 && bias_row < p.pen.n_bias ? p.pen.bias + (int64_t)bias_row * V : nullptr;
-  pen.allowed = mask_row >= 0 && mask_row < p.pen.n_allowed ? p.pen.allowed + (int64_t)mask_row * n_words : nullptr;
-  pen.rep = p.pen.repetition ? p.pen.repetition[q] : 1.0f, pen.pres = p.pen.presence ? p.pen.presence[q] : 0.0f;
-  pen.freq = p.pen.frequency ? p.pen.frequency[q] : 0.0f;
+  const RowPenalty pen = penalty_of(p.pen, q, me, V);
 
   words x[CHUNKS];
   uint32_t was_seen[CHUNKS] = {}, ok[CHUNKS];

@@ -13,6 +13,7 @@ constexpr int64_t kMaxSlots = 1 << 30;   // tokens of a cache, of a block table'
 constexpr int kMaxHeadEntries = 1 << 25;   // rows, or entries, of one call on rows of heads (a launch has fewer than 2^32 threads)
 
 constexpr int kMaxLogitsRows = (1 << 23) - 8;   // rows of one call on logits
+constexpr int kMaxSampledRows = 1 << 20, kMaxSampledBatch = 1 << 17;   // of one whose tokens are drawn
 
 // ---- attention of the rows over a paged cache and their own ancestors ----------------
 struct AttentionJob {
@@ -140,5 +141,36 @@ struct AcceptTreeJob {
   uint32_t* seen;
 };
 hipError_t launch_accept_tree(const AcceptTreeJob& job, hipStream_t st);
+
+// ---- verification against the target's probabilities ---------------------------------------
+struct SamplePart {        // of some of a row's tokens
+  float top;               // the largest processed logit
+  int32_t first;           // its first token
+  double sum;              // of the weights relative to it
+};
+struct SampleSlot {        // where a sequence's path has led
+  int32_t done, level, row;
+  int32_t tok[SPEC_MAX_STAGES], path[SPEC_MAX_STAGES];
+  float logp[SPEC_MAX_STAGES];
+};
+struct SampleJob {
+  const void* logits;
+  int batch, M, V, n;
+  spec_penalties_t pen;
+  int paths;               // whether a row's path counts
+  const int32_t *node_tok, *node_parent, *n_nodes;
+  const float *temperature, *uniform;
+  int32_t *accept_len, *out_tokens, *n_out, *path_row;
+  float* out_logp;
+  int32_t* counts;
+  uint32_t* seen;
+  // (the launch's)
+  int parts, span, all_rows;
+  SamplePart* part;        // of all rows, or of two rows of every sequence
+  float* node_v;
+  SampleSlot* slot;
+};
+int64_t sample_workspace(int batch, int M, int V, bool bf16);
+hipError_t launch_sample(SampleJob job, void* workspace, bool bf16, hipStream_t st);
 
 }  // namespace specdraft

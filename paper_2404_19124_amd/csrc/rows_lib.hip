@@ -475,3 +475,47 @@ extern "C" spec_status_t spec_verify_tree(const void* logits, int32_t logits_dty
   HIP_TRY(launch_accept_tree(a, st));
   return SPEC_OK;
 }
+
+static spec_status_t check_sampled(int32_t batch, int32_t M, int32_t vocab) {
+  // (a launch has fewer than 2^32 threads: 256 for each of up to 64 parts of a row of every sequence, or of the parts of few rows)
+  if (batch > kMaxSampledBatch || (int64_t)batch * (M + 1) > kMaxSampledRows)
+    return fail(SPEC_ESHAPE, "batch = %d exceeds %d, or batch * (M + 1) = %lld %d", batch, kMaxSampledBatch, (long long)batch * (M + 1), kMaxSampledRows);
+  return vocab > 1 << 30 ? fail(SPEC_ESHAPE, "vocab exceeds 2^30") : SPEC_OK;
+}
+
+extern "C" spec_status_t spec_verify_sampled_workspace(int32_t batch, int32_t M, int32_t vocab, int32_t logits_dtype, int64_t* bytes) {
+  if (!bytes) return fail(SPEC_EINVAL, "bytes is NULL");
+  if (!known_dtype(logits_dtype)) return fail(SPEC_EDTYPE, "logits_dtype = %d is neither SPEC_F32 nor SPEC_BF16", logits_dtype);
+  if (batch < 1 || M < 0 || vocab < 1) return fail(SPEC_EINVAL, "batch and vocab must be >= 1, M >= 0");
+  if (M > kMaxTreeItems) return fail(SPEC_ESHAPE, "M = %d exceeds %d", M, kMaxTreeItems);
+  spec_status_t s = check_sampled(batch, M, vocab);
+  if (s != SPEC_OK) return s;
+  *bytes = sample_workspace(batch, M, vocab, logits_dtype == SPEC_BF16);
+  return SPEC_OK;
+}
+
+extern "C" spec_status_t spec_verify_sampled(const void* logits, int32_t logits_dtype, const int32_t* node_tok, const int32_t* node_parent,
+                                             const int32_t* n_nodes, const spec_penalties_t* pen, const float* temperature,
+                                             const float* uniform, int32_t batch, int32_t M, int32_t n_predict, int32_t vocab,
+                                             int32_t* accept_len, int32_t* out_tokens, int32_t* n_out, int32_t* path_row, float* out_logp,
+                                             int32_t* counts_out, uint32_t* seen_out, void* workspace, int64_t workspace_bytes,
+                                             void* hip_stream) {
+  spec_status_t s = check_logits(logits, logits_dtype, batch, M, vocab, pen, node_tok, node_parent);
+  if (s == SPEC_OK) s = check_sampled(batch, M, vocab);
+  if (s != SPEC_OK) return s;
+  if (!uniform || !accept_len || !out_tokens || !n_out || !path_row) return fail(SPEC_EINVAL, "a required pointer is NULL");
+  if (M > 0 && (!node_tok || !node_parent)) return fail(SPEC_EINVAL, "node_tok or node_parent is NULL");
+  if (n_predict < 0 || n_predict > SPEC_MAX_STAGES) return fail(SPEC_EINVAL, "n_predict = %d outside [0, %d]", n_predict, SPEC_MAX_STAGES);
+  const int64_t need = sample_workspace(batch, M, vocab, logits_dtype == SPEC_BF16);
+  if (!workspace || workspace_bytes < need)
+    return fail(SPEC_EINVAL, "workspace of %lld bytes, needed are %lld", (long long)(workspace ? workspace_bytes : 0), (long long)need);
+  if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(SPEC_EINVAL, "workspace must be 16-byte aligned");
+  spec_penalties_t none = {};
+  SampleJob j = {};
+  j.logits = logits, j.batch = batch, j.M = M, j.V = vocab, j.n = n_predict, j.pen = pen ? *pen : none, j.paths = pen != nullptr;
+  j.node_tok = node_tok, j.node_parent = node_parent, j.n_nodes = n_nodes, j.temperature = temperature, j.uniform = uniform;
+  j.accept_len = accept_len, j.out_tokens = out_tokens, j.n_out = n_out, j.path_row = path_row, j.out_logp = out_logp;
+  j.counts = counts_out, j.seen = seen_out;
+  HIP_TRY(launch_sample(j, workspace, logits_dtype == SPEC_BF16, static_cast<hipStream_t>(hip_stream)));
+  return SPEC_OK;
+}
