@@ -440,8 +440,8 @@ spec_status_t spec_verify_tree(const void* logits, int32_t logits_dtype, const i
 
 /* VERIFY against the base model's probabilities (Sec. 1: speculative decoding keeps the base model's distribution), on the rows of the
  * tree, from given random numbers, with the penalties applied on the fly.  With v the processed logits of a row as spec_penalize gives
- * them in float32 (NaN taken as -inf), T = temperature[q] > 0 and, in 64 bits, w_t = exp((v_t - max v) / T) (where max v is infinite:
- * 1 for the infinite ones, 0 for others) and S their sum:
+ * them in float32 (NaN taken as -inf, +inf as the largest finite number), T = temperature[q] > 0 and, in 64 bits, w_t =
+ * exp((v_t - max v) / T) (nothing below 2^-1000) and S their sum:
  *     the row's mass S is laid out as the row's nodes' tokens in the order of their nodes (of siblings with the same token the first one,
  *     no token outside [0, vocab)), then all other tokens by number; its token is the one in whose stretch u * S lies, u =
  *     uniform[q][depth of the row] (taken as the nearest within [0, 1));

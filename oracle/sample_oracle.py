@@ -40,7 +40,8 @@ def processed(logits, s, row, node_tok, parent, pen):
 
 
 def weights(x, T):
-    """(w, their logarithms' shift) of processed logits; None where nothing is above -inf."""
+    """Weights of processed logits; None where nothing is above -inf.  (+inf is taken as the largest finite number.)"""
+    x = np.minimum(x, np.finfo(F).max)
     top = x.max()
     if top == -np.inf:
         return None
@@ -48,8 +49,6 @@ def weights(x, T):
         w = np.zeros(len(x))
         w[int(x.argmax())] = 1
         return w
-    if top == np.inf:
-        return (x == top).astype(np.float64)
     return np.exp((x.astype(np.float64) - float(top)) / float(F(T)))
 
 

@@ -145,13 +145,13 @@ hipError_t launch_accept_tree(const AcceptTreeJob& job, hipStream_t st);
 // ---- verification against the target's probabilities ---------------------------------------
 struct SamplePart {        // of some of a row's tokens
   float top;               // the largest processed logit
-  int32_t first;           // its first token
+  int32_t first;           // its first token, without a temperature
   double sum;              // of the weights relative to it
 };
 struct SampleSlot {        // where a sequence's path has led
-  int32_t done, level, row;
+  int32_t done, level, row, unused;
   int32_t tok[SPEC_MAX_STAGES], path[SPEC_MAX_STAGES];
-  float logp[SPEC_MAX_STAGES];
+  double weight[SPEC_MAX_STAGES], sum[SPEC_MAX_STAGES];   // the tokens' and their rows'
 };
 struct SampleJob {
   const void* logits;
@@ -165,7 +165,7 @@ struct SampleJob {
   int32_t* counts;
   uint32_t* seen;
   // (the launch's)
-  int parts, span, all_rows;
+  int parts, span, run, all_rows;
   SamplePart* part;        // of all rows, or of two rows of every sequence
   float* node_v;
   SampleSlot* slot;
