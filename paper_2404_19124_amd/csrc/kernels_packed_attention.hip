@@ -157,6 +157,388 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_attention_kerne
   attention_body<true, DP, MQ, WK, PackedCopy<DP, MQ, WK>>(p, ws, smem, s_valid, s_again);
 }
 
+// ---- few query rows: every wave goes through tiles of its own -----------------------------------------------------------------
+// A unit of up to 16 query rows has so little work for a key that a workgroup's barriers, not the bytes, would set the pace: here the
+// tiles of a segment go round the four waves, which meet at its end only.  Keys go from codes to the operand of the first product in
+// registers: lane l16 of group grp holds elements grp * DP/4 on of key l16 of a block of 16, and the queries lie in that order too.
+// Values pass through memory of the wave's own, 32 keys at a time, to be read transposed.
+constexpr int kStreamRows = 16;
+typedef __attribute__((address_space(1))) uint8_t global_u8;
+template <int DP>
+struct PackedStream {
+  typedef AttentionTile<true, DP, 1, 1> Tile;           // (its queries in another order)
+  static constexpr int NC = DP / 32, NS = DP > 128 ? 2 : 1;      // words of codes of a lane's quarter of a key, and scales
+  static constexpr int NB = KT / 16, ROWB = DP * 2, SWZ = ROWB / 16 < 16 ? ROWB / 16 - 1 : 15;
+  static constexpr int WAVE = 32 * ROWB, LDS = 4 * WAVE;         // memory of a wave
+  static_assert(3 * 64 * (DP / 4 + 2) * 4 <= LDS, "the waves' results fit their memory");
+  const AttentionJob& p;
+  int64_t to_v_rows;
+  int last_word;                                        // of a row of bfloat16
+  uint64_t k, v, k_scale, v_scale;                      // of the segment's head (what is the same in every lane is in scalar registers)
+  uint32_t offset[NS], scale_offset[NS];                // this lane's quarter of key l16 from a block's first key
+  uint32_t shift[NS];                                   // of its scale into a float's exponent; behind the head's elements away from it
+
+  // The blocks of 16 keys of 16 tiles from tile `base` on, one to a lane (pages hold whole ones): where they lie, and which of their
+  // keys are cached tokens.  What is none is read from the cache's first block, so that no read waits for a decision.
+  struct Places {
+    int64_t codes, scales;
+    int base;
+    uint32_t cached;
+  };
+  struct Codes {                                        // a tile's keys, or its values
+    uint32_t c[NB][NC];
+    uint32_t scale[NB][NS];
+  };
+
+  __device__ __forceinline__ void init() {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int e = grp * (DP / 4) + i * 32;
+      const bool ok = e < p.head_dim;
+      shift[i] = ok ? 23 : 31;   // (there the queries are zeros: any number will do, but for one that is not finite)
+      offset[i] = (uint32_t)(l16 * (int)p.slot + (ok ? e / 2 : 0));
+      scale_offset[i] = (uint32_t)(l16 * (int)p.scale_slot + (ok ? e / 32 : 0));
+    }
+  }
+  __device__ __forceinline__ void of(const Segment& s) {
+    k = uniform(reinterpret_cast<uint64_t>(s.k_cache));
+    v = k + (reinterpret_cast<uint64_t>(p.v) - reinterpret_cast<uint64_t>(p.k));
+    k_scale = uniform(reinterpret_cast<uint64_t>(p.k_scale + s.g * p.scale_head));
+    v_scale = k_scale + (reinterpret_cast<uint64_t>(p.v_scale) - reinterpret_cast<uint64_t>(p.k_scale));
+  }
+  __device__ __forceinline__ Places places(const Segment& s, int base) const {
+    const int key = (s.tile0 + base) * KT + (int)(threadIdx.x & 63) * 16;
+    Places r = {0, 0, base, 0};
+    if (key < s.ctx) {
+      const int b = key / p.block_size, x = p.block_table[(int64_t)s.q * p.max_blocks + b];
+      if (x >= 0 && x < p.n_blocks) {
+        const int slot = key - b * p.block_size;
+        r.codes = x * p.block + slot * p.slot, r.scales = x * p.scale_block + slot * p.scale_slot;
+        r.cached = (1u << min(s.ctx - key, 16)) - 1;
+      }
+    }
+    return r;
+  }
+  static __device__ __forceinline__ uint64_t of_lane(int64_t x, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+  }
+  // Requests tile t's keys, or its values; which of its keys are cached tokens.
+  __device__ __forceinline__ uint64_t load(int t, const Places& f, bool value, Codes& x) const {
+    uint64_t cached = 0;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int from = (t - f.base) * NB + nb;
+      cached |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane(f.cached, from) << nb * 16;
+      const global_u8* at = reinterpret_cast<const global_u8*>((value ? v : k) + of_lane(f.codes, from));
+      const global_u8* of = reinterpret_cast<const global_u8*>((value ? v_scale : k_scale) + of_lane(f.scales, from));
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        if constexpr (NC == 2) {
+          const uint64_t w = *reinterpret_cast<const __attribute__((address_space(1))) uint64_t*>(at + offset[i]);
+          x.c[nb][0] = (uint32_t)w, x.c[nb][1] = (uint32_t)(w >> 32);
+        } else {
+          const u32x4 w = *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(at + offset[i]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x.c[nb][i * 4 + k] = w[k];
+        }
+        x.scale[nb][i] = of[scale_offset[i]];
+      }
+    }
+    return cached;
+  }
+  // Block nb of a tile as bfloat16, this lane's quarter of key l16.  ROWS: some of the tile's keys are not cached tokens but rows of the
+  // tree, or none (then row 0)
+  template <bool ROWS>
+  __device__ __forceinline__ void expand(const Segment& s, int t, const Codes& x, int nb, uint64_t cached, bool value, bool careful, u32x4 (&w)[NC]) const {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) w[i] = unpack_scaled(x.c[nb][i], __uint_as_float(x.scale[nb][i * NS / NC] << shift[i * NS / NC]));
+    if constexpr (ROWS) {
+      const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
+      if (!((cached >> (nb * 16 + l16)) & 1)) {
+        const int key = (s.tile0 + t) * KT + nb * 16 + l16, row = key >= s.ctx && key < s.keys ? key - s.ctx : 0;
+        const uint8_t* from = s.k_rows + row * p.new_row + (value ? to_v_rows : 0) + grp * (DP / 4) * 2;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          w[i] = (u32x4){0, 0, 0, 0};
+          if (grp * (DP / 4) / 8 + i > last_word) continue;
+          w[i] = *reinterpret_cast<const u32x4*>(from + i * 16);
+          if (careful && value) {   // (see clean_tile)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((w[i][j] & 0x7f800000u) == 0x7f800000u) w[i][j] &= 0xffffu;
+              if ((w[i][j] & 0x7f80u) == 0x7f80u) w[i][j] &= 0xffff0000u;
+            }
+          }
+        }
+      }
+    }
+  }
+};
+
+template <int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(AttentionJob p, AttentionSpace ws) {
+  typedef PackedStream<DP> Stream;
+  typedef typename Stream::Tile Tile;
+  constexpr int BM = kStreamRows, NB = Stream::NB, NC = Stream::NC, ND = DP / 16, ROWB = Stream::ROWB;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  __shared__ uint32_t s_again;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, grp = lane >> 4;
+  const int G = p.q_heads / p.kv_heads;
+  Schedule<BM, unit_cost(true)> plan = {p, G};
+  if (!plan.live(ws)) return;
+  Segment now;
+  Owner mine = {-1, 0, 0, 0, 0};
+  bool more = plan.first(now);
+  if (!more) {
+    if (tid == 0) ws.owner[plan.me] = mine;
+    return;
+  }
+  const int me = plan.me;
+  const float q_sign = p.scale < 0 ? -1.0f : p.scale == 0 ? 0.0f : 1.0f;
+  const float sc = (p.scale == 0 ? 1.0f : fabsf(p.scale)) * kLog2e;
+  Stream in = {p, static_cast<const uint8_t*>(p.v_new) - static_cast<const uint8_t*>(p.k_new), p.head_dim / 8 - 1};
+  in.init();
+  uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + Stream::LDS);
+  lds_u8* vb = (lds_u8*)smem + wave * Stream::WAVE;
+  bool careful = false;        // the second pass over this share
+  int n_units = 0, first_odd = 1 << 30, unit0 = 0;   // as in attention_body
+  if (tid == 0) s_again = 0;
+  while (more) {
+    const int rows = (now.nodes + 1) * G - now.block * BM;
+    const bool holds_rows = (now.tile0 + now.n_tiles) * KT > now.ctx;
+    if (holds_rows)
+      for (int i = tid; i < now.keys - now.ctx - 1; i += 256) {
+        const int up = p.node_parent[(int64_t)now.q * p.M + i];
+        s_up[i + 1] = (uint16_t)(up >= 0 && up < i ? up + 1 : 0);
+      }
+    Tile x;
+    const int mm = l16 < rows ? now.block * BM + l16 : 0;
+    x.row_of[0] = mm / G;
+    const uint8_t* from = static_cast<const uint8_t*>(p.q) + now.q * p.q_seq + (int64_t)x.row_of[0] * p.q_row + (int64_t)(now.g * G + mm % G) * p.q_head;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int word = grp * NC + i;
+      u32x4 raw = {0, 0, 0, 0};
+      if (word <= in.last_word) raw = *reinterpret_cast<const u32x4*>(from + word * 16);
+      if (q_sign != 1.0f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw[j] = q_sign == 0.0f ? 0u : raw[j] ^ 0x80008000u;
+      }
+      x.qf[0][i] = __builtin_bit_cast(bf16x8, raw);
+    }
+    float m_run = kLowest, l_run = 0;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) x.o[0][d] = (f32x4){0, 0, 0, 0};
+    in.of(now);
+    const int n_tiles = uniform(now.n_tiles);
+    typename Stream::Places f = in.places(now, 0);
+    typename Stream::Codes kc, vc;
+    uint64_t cached = 0;
+    bool odd = false;
+    __syncthreads();   // parents are there; the last segment's results have been read
+    auto tile = [&](auto has_rows, int t) {
+      constexpr bool ROWS = decltype(has_rows)::value;
+      const int t0 = (now.tile0 + t) * KT, ctx = now.ctx;
+      const uint64_t here = cached;
+      // ---- scores, transposed: keys 4 grp + i of a block in the lane's registers, query row l16 ----
+      f32x4 s[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        u32x4 kf[NC];
+        in.template expand<ROWS>(now, t, kc, nb, here, false, careful, kf);
+        s[nb] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < NC; ++st) s[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[st]), x.qf[0][st], s[nb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const int next = t + 4 < n_tiles ? t + 4 : t;   // (behind its last tile a wave requests that again: no decision)
+      if constexpr (!ROWS) {
+        if (next - f.base >= 16) f = in.places(now, next);
+        cached = in.load(next, f, false, kc);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        uint64_t sees = here;
+        int row = x.row_of[0];
+        auto see = [&](int r) {
+          const uint32_t bit = (uint32_t)(ctx + r - t0);
+          if (bit < (uint32_t)KT) sees |= 1ull << bit;
+        };
+        if (t0 + KT > ctx) {
+          for (int i = 0; i < kMaxStages && row > 0; ++i) {
+            see(row);
+            row = s_up[row];
+          }
+          see(0);
+        }
+        sees >>= grp * 4;
+        const uint32_t word[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!((word[nb / 2] >> ((nb & 1) * 16 + i)) & 1)) s[nb][i] = SPEC_NEG_INF;
+      }
+      // ---- softmax: weights relative to a bound of the scores ----
+      float top = s[0][0];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nb][i]);
+      top = groups_max(top) * sc;
+      if (__any(top > m_run)) {
+        const float m_new = fmaxf(m_run, top + kSlack), keep = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= keep;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x.o[0][d][i] *= keep;
+      }
+      bf16x8 w[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 raw;
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          float e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * h + nb][i], sc, -m_run));
+          raw[2 * nb] = f32_to_bf16_pair(e[0], e[1]), raw[2 * nb + 1] = f32_to_bf16_pair(e[2], e[3]);
+        }
+        // (the sum is that of the weights as they are multiplied)
+        const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t pair = raw[i];   // (of its own: a bit_cast of a vector's element takes the first one)
+          l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, l_run, false);
+        }
+        w[h] = __builtin_bit_cast(bf16x8, raw);
+      }
+      // ---- values, 32 keys at a time (a wave's reads and writes of LDS keep their order) ----
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          u32x4 vf[NC];
+          in.template expand<ROWS>(now, t, vc, 2 * h + nb, here, true, careful, vf);
+          const int key = nb * 16 + l16;
+#pragma unroll
+          for (int i = 0; i < NC; ++i) *reinterpret_cast<lds_u32x4*>(vb + key * ROWB + (((grp * NC + i) ^ (key & Stream::SWZ)) * 16)) = vf[i];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (h == 1 && !ROWS) in.load(next, f, true, vc);
+        __builtin_amdgcn_sched_barrier(0);
+        i16x4 v[3][2];   // (two steps' reads are under way)
+        auto read = [&](int d) {
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) {
+            const int key = nb * 16 + grp * 4 + (l16 >> 2), word = (d * 2 + ((l16 & 3) >> 1)) ^ (key & Stream::SWZ);
+            v[d % 3][nb] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + key * ROWB + word * 16 + (l16 & 1) * 8));
+          }
+        };
+        read(0);
+        read(1);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          if (d + 2 < ND) read(d + 2);
+          __builtin_amdgcn_sched_barrier(0);
+          const i16x4 a = v[d % 3][0], b = v[d % 3][1];
+          x.o[0][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (i16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}), w[h], x.o[0][d], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    // tiles of cached tokens, each requested while the one before is worked on; the others, a share's last ones, when it is their turn
+#pragma unroll 1
+    for (int t = wave; t < n_tiles; t += 4) {
+      if (t - f.base >= 16) f = in.places(now, t);
+      cached = in.load(t, f, false, kc);
+      __builtin_amdgcn_sched_barrier(0);
+      in.load(t, f, true, vc);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+      for (; cached == ~0ull && t < n_tiles; t += 4) tile(std::false_type(), t);
+      if (t >= n_tiles) break;
+      odd = true;
+      tile(std::true_type(), t);
+    }
+    l_run = groups_sum(l_run);
+
+    // ---- join of the waves ----
+    float* box = reinterpret_cast<float*>(smem);
+    constexpr int PER = DP / 4 + 2;
+    odd = __syncthreads_or(odd);
+    if (wave > 0) {
+      float* to = box + (wave - 1) * PER * 64 + lane;
+      to[0] = m_run;
+      to[64] = l_run;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[(2 + d * 4 + i) * 64] = x.o[0][d][i];
+    }
+    __syncthreads();
+    const bool whole = now.n_seg == now.tiles;
+    if (!whole && now.tile0 == 0) mine = {now.q, now.g, now.block, plan.last(), min(rows, BM)};
+    if (wave == 0) {
+      for (int y = 0; y < 3; ++y) {
+        const float* of = box + y * PER * 64 + lane;
+        const float m = of[0], m_new = fmaxf(m, m_run);
+        const float ours = __builtin_amdgcn_exp2f(m_run - m_new), its = __builtin_amdgcn_exp2f(m - m_new);
+        m_run = m_new;
+        l_run = l_run * ours + of[64] * its;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x.o[0][d][i] = x.o[0][d][i] * ours + of[(2 + d * 4 + i) * 64] * its;
+      }
+      if (odd && !careful) {
+        float zero = 0;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x.o[0][d][i], 0.0f, zero);
+        if (__any(!(zero == 0.0f))) {
+          if (lane == 0) s_again = 1;
+          first_odd = min(first_odd, n_units);
+        }
+      }
+      if (careful && holds_rows)
+        add_left_out(x, now.k_rows, in.to_v_rows, p.new_row, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, s_up, in.last_word);
+      if (l16 < rows && (careful ? n_units - unit0 >= first_odd : n_units < first_odd)) {
+        if (whole) {
+          const float inv = 1.0f / l_run;
+          uint8_t* to = static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)x.row_of[0] * p.out_row + (int64_t)(now.g * G + mm % G) * p.out_head;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            const int e = d * 16 + grp * 4;
+            if (e < p.head_dim) {
+              const f32x4 v = x.o[0][d] * inv;
+              *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(v[2], v[3]) << 32 | f32_to_bf16_pair(v[0], v[1]);
+            }
+          }
+        } else {
+          float* to = ws.part + ((int64_t)(me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + l16) * (DP + 4);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + d * 16 + grp * 4) = x.o[0][d];
+          if (grp == 0) to[DP] = m_run, to[DP + 1] = l_run;
+        }
+      }
+    }
+    more = plan.following(now);
+    if (more) plan.advance(now);
+    ++n_units;
+    __syncthreads();   // the results and the parents have been read
+    if (!more && !careful && s_again) {
+      careful = true;
+      unit0 = n_units;
+      more = plan.first(now);
+    }
+  }
+  if (tid == 0) ws.owner[me] = mine;
+}
+
 template <int DP, int MQ, int WK>
 static hipError_t launch_packed_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
   typedef AttentionShape<true, DP, MQ, WK> S;
@@ -179,7 +561,43 @@ static hipError_t launch_packed_t(const AttentionJob& job, const AttentionPlan& 
   return hipGetLastError();
 }
 
+template <int DP>
+static hipError_t launch_stream_t(const AttentionJob& job, const AttentionPlan& plan, hipStream_t st) {
+  const AttentionSpace ws = space_of(job, plan);
+  const size_t smem = PackedStream<DP>::LDS + (((size_t)job.M + 8) & ~(size_t)7) * sizeof(uint16_t);
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  static std::atomic<uint64_t> allowed{0};   // devices where this kernel may have so much memory, per instantiation
+  if (device >= 64 || !((allowed.load(std::memory_order_relaxed) >> device) & 1)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(packed_stream_kernel<DP>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            PackedStream<DP>::LDS + ((kMaxTreeItems + 8) & ~7) * (int)sizeof(uint16_t));
+    if (e != hipSuccess) return e;
+    if (device < 64) allowed.fetch_or(1ull << device, std::memory_order_relaxed);
+  }
+  hipLaunchKernelGGL((packed_stream_kernel<DP>), dim3(plan.groups), dim3(256), smem, st, job, ws);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attention_join_kernel<true, DP, kStreamRows>), dim3(plan.groups, (kStreamRows + join_rows(DP) - 1) / join_rows(DP)), dim3(256), 0, st, job, ws);
+  return hipGetLastError();
+}
+
+// (the body's shares need no more workspace)
+static AttentionPlan plan_stream(int M, int q_heads, int kv_heads, int head_dim) {
+  AttentionPlan a = plan_attention(M, q_heads, kv_heads, head_dim, true);
+  if (a.bm == kStreamRows) a.groups = a.dp <= 128 ? 512 : 256, a.least = 4;
+  return a;
+}
+
+int64_t packed_attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim) {
+  const AttentionPlan a = plan_stream(M, q_heads, kv_heads, head_dim);
+  return owner_bytes(a.groups) + (int64_t)a.groups * 2 * a.bm * (a.dp + 4) * 4;
+}
+
 hipError_t launch_packed_attention(const AttentionJob& job, hipStream_t st) {
+  const AttentionPlan few = plan_stream(job.M, job.q_heads, job.kv_heads, job.head_dim);
+  if (few.bm == kStreamRows && job.one_place)
+    return few.dp == 64 ? launch_stream_t<64>(job, few, st) : few.dp == 128 ? launch_stream_t<128>(job, few, st) : launch_stream_t<256>(job, few, st);
   const AttentionPlan a = plan_attention(job.M, job.q_heads, job.kv_heads, job.head_dim, true);
 #define LAUNCH(DP, BM, MQ, WK) \
   if (a.dp == DP && a.bm == BM) return launch_packed_t<DP, MQ, WK>(job, a, st)
