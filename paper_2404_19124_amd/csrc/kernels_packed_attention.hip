@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_attention_kerne
 // tiles of a segment go round the four waves, which meet at its end only.  Keys go from codes to the operand of the first product in
 // registers: lane l16 of group grp holds elements grp * DP/4 on of key l16 of a block of 16, and the queries lie in that order too.
 // Values pass through memory of the wave's own, 32 keys at a time, to be read transposed.
-constexpr int kStreamRows = 16;
+constexpr int kStreamRows = 16, kStreamCost = 12;   // (cost of a unit, in tiles)
 typedef __attribute__((address_space(1))) uint8_t global_u8;
 template <int DP>
 struct PackedStream {
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(A
   __shared__ uint32_t s_again;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, grp = lane >> 4;
   const int G = p.q_heads / p.kv_heads;
-  Schedule<BM, unit_cost(true)> plan = {p, G};
+  Schedule<BM, kStreamCost> plan = {p, G};
   if (!plan.live(ws)) return;
   Segment now;
   Owner mine = {-1, 0, 0, 0, 0};
