@@ -427,12 +427,22 @@ struct Schedule {
   // false: this workgroup has no share
   __device__ __forceinline__ bool live(const AttentionSpace& ws) {
     const int lane = threadIdx.x & 63;
-    all = 0;
-    for (int q0 = 0; q0 < p.batch; q0 += 64) {
-      uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, COST).total : 0;
+    // costs of 64 sequences, and of each with those before it
+    auto costs = [&](int q0, uint64_t& t, uint64_t& sum) {
+      t = sum = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, COST).total : 0;
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) t += __shfl_xor((unsigned long long)t, d);
-      all += t;
+      for (int d = 1; d < 64; d *= 2) {
+        const uint64_t y = __shfl_up((unsigned long long)sum, d);
+        if (lane >= d) sum += y;
+      }
+    };
+    uint64_t t0, sum0;
+    costs(0, t0, sum0);
+    all = __shfl((unsigned long long)sum0, 63);
+    for (int q0 = 64; q0 < p.batch; q0 += 64) {
+      uint64_t t, sum;
+      costs(q0, t, sum);
+      all += __shfl((unsigned long long)sum, 63);
     }
     all = uniform(all);
     groups = min((uint64_t)(all <= kFewCost * 256 ? 256 : ws.groups), (all + ws.least - 1) / ws.least);
@@ -447,12 +457,8 @@ struct Schedule {
     q = 0;
     start = 0;
     for (int q0 = 0; q0 < p.batch; q0 += 64) {   // (lengths that change under way end the search, and the work, early)
-      uint64_t t = q0 + lane < p.batch ? seq_tiles(p, q0 + lane, BM, COST).total : 0, sum = t;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint64_t y = __shfl_up((unsigned long long)sum, d);
-        if (lane >= d) sum += y;
-      }
+      uint64_t t = t0, sum = sum0;
+      if (q0 > 0) costs(q0, t, sum);
       const uint64_t over = __ballot(start + sum > at);
       if (over) {
         const int l = __ffsll((unsigned long long)over) - 1;
