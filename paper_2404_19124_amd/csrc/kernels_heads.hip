@@ -205,29 +205,27 @@ hipError_t launch_heads(HeadsJob job, bool bf16, bool append, hipStream_t st) {
 // A group of 32 elements has a scale 2^e, e the smallest with (largest amount) <= 7 * 2^e, within [-125, 125]: what is above 6 * 2^e is
 // then off by half a step at most, as if the amounts went on.  Codes are rounded to the nearest amount, of two as near to the even code.
 
-// Scale byte and codes of 32 elements.
-__device__ __forceinline__ uint32_t pack_group(const float (&x)[32], u32x4& codes) {
+// Scale byte of a group, four lanes with eight elements each, and the codes of this lane's.
+__device__ __forceinline__ uint32_t pack_group(const float (&x)[8], uint32_t& codes) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  codes = (u32x4){0, 0, 0, 0};
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, true));   // lanes 1 0 3 2 of the four
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, true));   // lanes 2 3 0 1
+  codes = 0;
   if (top >= 0x7f800000u) return 255;   // an infinity or NaN: no element of the group is a number
   const int e = min(max((int)(top >> 23) - 129 + ((top & 0x7fffffu) > 0x600000u), -125), 125);
   const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * i], x[8 * i + 1], scale, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * i + 2], x[8 * i + 3], scale, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * i + 4], x[8 * i + 5], scale, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * i + 6], x[8 * i + 7], scale, 3);
-    codes[i] = w;
-  }
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
   return (uint32_t)(e + 127);
 }
 
-// A lane takes a group of 32 elements of a head: what it packs is in its registers.  The other elements of its pairs it reads again, from
-// the cache where its neighbours' reads have brought them.
+// A lane takes a word of a head, eight elements, four lanes a group of 32: a wave reads 1 KiB and writes 256 bytes in a row.  The other
+// elements of its pairs it reads again, from the cache where its neighbours' reads have brought them.  Memory bounds it: 16,000 tokens of 8
+// heads of 128 with their norms, rotation and tables, 91 MB, 26 us, 3.5 TB/s (a whole group to a lane, 64 bytes apart: 53 us).
 template <bool PAIRS>
 __global__ __launch_bounds__(256) void pack_kernel(PackJob p) {
   typedef HeadWord<true> Word;
@@ -236,72 +234,49 @@ __global__ __launch_bounds__(256) void pack_kernel(PackJob p) {
   const int slot = p.slot[t], src = p.src_row ? p.src_row[t] : t, pos = p.cos ? p.pos[t] : 0;
   if (slot < 0 || slot >= p.n_slots || src < 0 || src >= p.rows || (p.cos && (pos < 0 || pos >= p.n_pos))) return;
   const int block = slot / p.block_size, in = slot - block * p.block_size;
-  const int group = lane & (p.lanes - 1), per = 64 / p.lanes, turned_words = 2 * p.half_words;
-  const bool active = group < p.groups;
+  const int word = lane & (p.lanes - 1), per = 64 / p.lanes;
+  const bool active = word < p.groups * 4, turned = word < 2 * p.half_words, first = word < p.half_words;
+  const int other = !turned || PAIRS ? word : first ? word + p.half_words : word - p.half_words;
+  Word c, s;
+  if (turned) {
+    const int64_t at = (int64_t)pos * p.half_words * 8;
+    if constexpr (PAIRS) load_half<true>(c, p.cos + at + word * 4), load_half<true>(s, p.sin + at + word * 4);
+    else c.load(p.cos + at + min(word, other) * 8), s.load(p.sin + at + min(word, other) * 8);
+  }
   const int side_trips = (p.heads + per - 1) / per;
   for (int trip = blockIdx.y * p.trips; trip < min(2 * side_trips, (int)(blockIdx.y + 1) * p.trips); ++trip) {
     const bool key = trip < side_trips;
     const int head = (key ? trip : trip - side_trips) * per + lane / p.lanes;
     const bool mine = active && head < p.heads;
     const uint8_t* from = (key ? p.k_new : p.v_new) + layer * p.new_layer + src * p.new_row + head * p.new_head;
-    Word x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i].from(mine ? *reinterpret_cast<const u32x4*>(from + (group * 4 + i) * 16) : (u32x4){0, 0, 0, 0});
-    float inv = 1;
-    const float* weight = p.weight && key ? p.weight + (int64_t)layer * p.groups * 32 : nullptr;
-    if (weight) {
-      inv = head_factor(lanes_sum((x[0].squares() + x[1].squares()) + (x[2].squares() + x[3].squares()), p.lanes), p.groups * 32, p.eps);
-      if (mine) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          Word w;
-          w.load(weight + (group * 4 + i) * 8);
-          x[i].scale(inv, w);
-        }
-      }
+    u32x4 rx = {0, 0, 0, 0}, ry = {0, 0, 0, 0};
+    if (mine) rx = *reinterpret_cast<const u32x4*>(from + word * 16);
+    if (!PAIRS && mine && key && turned) ry = *reinterpret_cast<const u32x4*>(from + other * 16);
+    Word x, y;
+    x.from(rx), y.from(ry);
+    if (p.weight && key) {
+      const float inv = head_factor(lanes_sum(x.squares(), p.lanes), p.groups * 32, p.eps);
+      const float* weight = p.weight + (int64_t)layer * p.groups * 32;
+      Word w;
+      if (active) w.load(weight + word * 8), x.scale(inv, w);
+      if (!PAIRS && active && turned) w.load(weight + other * 8), y.scale(inv, w);
     }
-    if (mine && key) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int word = group * 4 + i;
-        if (word >= turned_words) continue;
-        Word c, s;
-        if constexpr (PAIRS) {
-          const int64_t at = (int64_t)pos * p.half_words * 8 + word * 4;
-          load_half<true>(c, p.cos + at), load_half<true>(s, p.sin + at);
-          turn_pairs<true>(x[i], c, s);
-        } else {
-          const bool first = word < p.half_words;
-          const int other = first ? word + p.half_words : word - p.half_words;
-          const int64_t at = (int64_t)pos * p.half_words * 8 + min(word, other) * 8;
-          c.load(p.cos + at), s.load(p.sin + at);
-          Word y;
-          y.from(*reinterpret_cast<const u32x4*>(from + other * 16));
-          if (weight) {
-            Word w;
-            w.load(weight + other * 8);
-            y.scale(inv, w);
-          }
-          if (first) turn<true>(x[i], y, c, s);
-          else turn<true>(y, x[i], c, s);
-        }
-      }
+    if (turned && key) {
+      if constexpr (PAIRS) turn_pairs<true>(x, c, s);
+      else if (first) turn<true>(x, y, c, s);
+      else turn<true>(y, x, c, s);
     }
-    if (!mine) continue;
-    float v[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = x[i / 8].x[i % 8];
-    u32x4 codes;
-    const uint32_t scale = pack_group(v, codes);
-    const int64_t to = layer * p.layer + block * p.block + in * p.slot_stride + head * p.head + group * 16;
-    const int64_t at = layer * p.scale_layer + block * p.scale_block + in * p.scale_slot + head * p.scale_head + group;
-    *reinterpret_cast<u32x4*>((key ? p.k : p.v) + to) = codes;
-    (key ? p.k_scale : p.v_scale)[at] = (uint8_t)scale;
+    uint32_t codes;
+    const uint32_t scale = pack_group(x.x, codes);
+    const int64_t to = layer * p.layer + block * p.block + in * p.slot_stride + head * p.head + word * 4;
+    const int64_t at = layer * p.scale_layer + block * p.scale_block + in * p.scale_slot + head * p.scale_head + word / 4;
+    if (mine) *reinterpret_cast<uint32_t*>((key ? p.k : p.v) + to) = codes;
+    if (mine && word % 4 == 0) (key ? p.k_scale : p.v_scale)[at] = (uint8_t)scale;
   }
 }
 
 hipError_t launch_pack(PackJob job, hipStream_t st) {
-  job.lanes = power_of_two(job.groups);
+  job.lanes = power_of_two(job.groups * 4);
   const int per = 64 / job.lanes, trips = 2 * ((job.heads + per - 1) / per);
   job.trips = trips_of_a_wave(trips, (int64_t)job.entries * job.layers);
   const dim3 grid((unsigned)((job.entries + 3) / 4), (unsigned)((trips + job.trips - 1) / job.trips), (unsigned)job.layers);
@@ -310,7 +285,10 @@ hipError_t launch_pack(PackJob job, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Eight elements of a key and of a value per thread and turn.
+// Eight elements of a key and of a value per thread and turn.  What bounds it is memory, 3.8 bytes written for each one read: stores that the
+// caches do not keep take 60,000 tokens of 8 heads of 128 from 76 to 52 us (4.1 -> 6.0 TB/s), with a sum over the rows behind it from 76 to
+// 66 us at 125 MiB and from 163 to 160 at 250; below 32 MiB the two are the same.  (Rows rotated so are faster by themselves, 42 -> 41 us at
+// 125 MiB, but with their reader slower, 81 -> 92.)
 __global__ __launch_bounds__(256) void unpack_kernel(UnpackJob p) {
   const int per = p.heads * p.groups * 4, layer = blockIdx.y;
   const int64_t total = (int64_t)p.count * per;
@@ -322,8 +300,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(UnpackJob p) {
     const int64_t from = layer * p.layer + block * p.block + in * p.slot_stride + h * p.head + c * 4;
     const int64_t at = layer * p.scale_layer + block * p.scale_block + in * p.scale_slot + h * p.scale_head + c / 4;
     const int64_t to = layer * p.out_layer + t * p.out_row + h * p.out_head + c * 16;
-    *reinterpret_cast<u32x4*>(p.k_out + to) = unpack_word(*reinterpret_cast<const uint32_t*>(p.k + from), p.k_scale[at]);
-    *reinterpret_cast<u32x4*>(p.v_out + to) = unpack_word(*reinterpret_cast<const uint32_t*>(p.v + from), p.v_scale[at]);
+    __builtin_nontemporal_store(unpack_word(*reinterpret_cast<const uint32_t*>(p.k + from), p.k_scale[at]), reinterpret_cast<u32x4*>(p.k_out + to));
+    __builtin_nontemporal_store(unpack_word(*reinterpret_cast<const uint32_t*>(p.v + from), p.v_scale[at]), reinterpret_cast<u32x4*>(p.v_out + to));
   }
 }
 
