@@ -592,18 +592,20 @@ __global__ __launch_bounds__(kSampleThreads, 3) void sample_walk_kernel(SampleJo
   if (tid < 64) emit(p, q, s, token, weight, s_set.sum);
 }
 
-// Logits of so many bytes are read whole rather than row by row down the paths.
-constexpr int64_t kAllRowsBytes = 32 << 20;
+// Up to so many logits are all taken in one launch, more row by row down the paths, a launch for each depth.  All rows / paths, us: trees of
+// 49 rows, vocabulary 32,000, float32, 1, 8, 16 and 32 sequences (1.6, 13, 25 and 50 million logits) 24.5 / 30.6, 42.4 / 58.4, 60.6 / 65.1 and
+// 95.2 / 68.5; of 65 rows, 128,256, bfloat16, 1, 2, 4 and 8 sequences (8, 17, 33 and 67 million) 37.1 / 43.9, 49.1 / 47.1, 70.0 / 51.9 and 111 / 65.0.
+constexpr int64_t kAllRowsLogits = 1 << 24;
 
 struct SamplePlan {
   int parts, span, run;   // tokens of a part, and of a thread of it
   bool all_rows;
   int64_t part_bytes, node_bytes, slot_bytes;
 };
-static SamplePlan plan_sample(int batch, int M, int V, bool bf16) {
+static SamplePlan plan_sample(int batch, int M, int V) {
   SamplePlan a;
   const int64_t rows = (int64_t)batch * (M + 1);
-  a.all_rows = M == 0 || rows * V * (bf16 ? 2 : 4) <= kAllRowsBytes;
+  a.all_rows = M == 0 || rows * V <= kAllRowsLogits;
   const int64_t least = ((int64_t)V + kMaxParts * kSampleThreads - 1) / (kMaxParts * kSampleThreads);   // tokens of a thread
   a.run = (int)max((int64_t)16, (least + 15) & ~(int64_t)15);
   a.span = a.run * kSampleThreads;
@@ -615,13 +617,13 @@ static SamplePlan plan_sample(int batch, int M, int V, bool bf16) {
   return a;
 }
 
-int64_t sample_workspace(int batch, int M, int V, bool bf16) {
-  const SamplePlan a = plan_sample(batch, M, V, bf16);
+int64_t sample_workspace(int batch, int M, int V) {
+  const SamplePlan a = plan_sample(batch, M, V);
   return a.part_bytes + a.node_bytes + a.slot_bytes;
 }
 
 hipError_t launch_sample(SampleJob job, void* workspace, bool bf16, hipStream_t st) {
-  const SamplePlan a = plan_sample(job.batch, job.M, job.V, bf16);
+  const SamplePlan a = plan_sample(job.batch, job.M, job.V);
   job.parts = a.parts, job.span = a.span, job.run = a.run, job.all_rows = a.all_rows;
   uint8_t* at = static_cast<uint8_t*>(workspace);
   job.part = reinterpret_cast<SamplePart*>(at);

@@ -171,7 +171,7 @@ struct SampleJob {
   float* node_v;
   SampleSlot* slot;
 };
-int64_t sample_workspace(int batch, int M, int V, bool bf16);
+int64_t sample_workspace(int batch, int M, int V);
 hipError_t launch_sample(SampleJob job, void* workspace, bool bf16, hipStream_t st);
 
 }  // namespace specdraft

@@ -491,7 +491,7 @@ extern "C" spec_status_t spec_verify_sampled_workspace(int32_t batch, int32_t M,
   if (M > kMaxTreeItems) return fail(SPEC_ESHAPE, "M = %d exceeds %d", M, kMaxTreeItems);
   spec_status_t s = check_sampled(batch, M, vocab);
   if (s != SPEC_OK) return s;
-  *bytes = sample_workspace(batch, M, vocab, logits_dtype == SPEC_BF16);
+  *bytes = sample_workspace(batch, M, vocab);
   return SPEC_OK;
 }
 
@@ -507,7 +507,7 @@ extern "C" spec_status_t spec_verify_sampled(const void* logits, int32_t logits_
   if (!uniform || !accept_len || !out_tokens || !n_out || !path_row) return fail(SPEC_EINVAL, "a required pointer is NULL");
   if (M > 0 && (!node_tok || !node_parent)) return fail(SPEC_EINVAL, "node_tok or node_parent is NULL");
   if (n_predict < 0 || n_predict > SPEC_MAX_STAGES) return fail(SPEC_EINVAL, "n_predict = %d outside [0, %d]", n_predict, SPEC_MAX_STAGES);
-  const int64_t need = sample_workspace(batch, M, vocab, logits_dtype == SPEC_BF16);
+  const int64_t need = sample_workspace(batch, M, vocab);
   if (!workspace || workspace_bytes < need)
     return fail(SPEC_EINVAL, "workspace of %lld bytes, needed are %lld", (long long)(workspace ? workspace_bytes : 0), (long long)need);
   if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(SPEC_EINVAL, "workspace must be 16-byte aligned");

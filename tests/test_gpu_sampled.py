@@ -120,7 +120,7 @@ def test_penalties_one_by_one(pen, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_rows_are_taken_depth_by_depth(dtype):
-    """Logits of more than 32 MiB, against the oracle and against the same sequences by themselves: the bits are the same."""
+    """More than 2^24 logits, against the oracle and against the same sequences by themselves: the bits are the same."""
     c = Case(9, 40, 70001, 5, dtype, seed=8, share=0.8, n_nodes=[40, 39, -1, 7, 0, 40, 20, 40, 11])
     a = c.run(update=True)
     assert max(int(x) for x in a["accept_len"]) >= 3
