@@ -286,7 +286,7 @@ hipError_t launch_pack(PackJob job, hipStream_t st) {
 }
 
 // Eight elements of a key and of a value per thread and turn.  What bounds it is memory, 3.8 bytes written for each one read: stores that the
-// caches do not keep take 60,000 tokens of 8 heads of 128 from 76 to 52 us (4.1 -> 6.0 TB/s), with a sum over the rows behind it from 76 to
+// caches do not keep take 60,000 tokens of 8 heads of 128 from 76 to 52 us (4.1 -> 6.0 TB/s), with a reader of the rows behind it from 76 to
 // 66 us at 125 MiB and from 163 to 160 at 250; below 32 MiB the two are the same.  (Rows rotated so are faster by themselves, 42 -> 41 us at
 // 125 MiB, but with their reader slower, 81 -> 92.)
 __global__ __launch_bounds__(256) void unpack_kernel(UnpackJob p) {
