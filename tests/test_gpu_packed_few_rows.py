@@ -1,0 +1,177 @@
+"""spec_packed_attention with up to 16 query rows for a key head, where a kernel of its own takes pages of a multiple of 16 tokens: what may
+lie where nothing is read, places out of range, strides, infinities, streams and graphs."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2404_19124_amd import binding as B
+from tests.rows_common import dev
+from tests.test_gpu_packed_attention import PackedCase
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 160, 256])
+def test_idle_sequences_and_what_lies_behind_lengths_and_rows(D):
+    c = PackedCase(4, 2, D, 32, 7, [50, 100, 1, 0, 70, 250], seed=31, n_nodes=[-1, 0, 7, 3, -1, 5])
+    for q, n in enumerate(c.n_nodes):
+        for t in (c.q, c.k_new, c.v_new):
+            t[q, n + 1:] = float("nan")
+    c.table[0] = -5
+    c.parent[0] = 1 << 20
+    for q, n in enumerate(c.ctx):
+        if q and n % 32:
+            for s in c.scales:
+                s[c.table[q, n // 32], n % 32:] = 255
+    used = set(int(x) for q, n in enumerate(c.ctx) if q for x in c.table[q, :-(-n // 32)])
+    for x in set(range(c.k.shape[0])) - used:      # (the first block among them or not)
+        c.scales[0][x], c.scales[1][x] = 255, 255
+    c.values()
+    c.check_both()
+
+
+def test_a_first_block_of_nothing_but_nan():
+    """Block 0 is nobody's, and no number."""
+    c = PackedCase(2, 2, 128, 16, 4, [40, 3, 0, 130], seed=32)
+    n = c.k.shape[0]
+    free = next(x for x in range(n) if x not in set(c.table[c.table >= 0].tolist()))
+    for t in (*c.codes, *c.scales):
+        t[[0, free]] = t[[free, 0]]
+    c.table = np.where(c.table == 0, free, c.table)
+    for s in c.scales:
+        s[0] = 255
+    c.values()
+    c.check_both()
+
+
+@pytest.mark.parametrize("D", [64, 128, 192])
+def test_blocks_and_lengths_out_of_range(D):
+    c = PackedCase(4, 2, D, 16, 6, [200, 64, 40, 500], seed=33)
+    c.table[0, 2], c.table[0, 7], c.table[0, 12] = -1, c.k.shape[0], 2 ** 31 - 1
+    c.table[1, :] = -(2 ** 31)
+    c.table[3, 3:9] = -1
+    c.check_both()
+    c = PackedCase(4, 2, D, 16, 6, [32, 48, 16], seed=34)
+    wild = c.packed(ctx_len=dev(np.array([32, -9, 16], np.int32)), n_nodes=dev(np.array([-7, 6, 1 << 30], np.int32)))
+    c.ctx, c.n_nodes = np.array([32, 0, 16], np.int32), np.array([-1, 6, 6], np.int32)
+    c.check(wild)
+
+
+def test_strides():
+    """Rows out of one product, one layer of a cache with keys and values side by side in a block, an output inside a wider buffer."""
+    c = PackedCase(6, 2, 64, 16, 4, [100, 31, 0, 300], seed=35)
+    fused = torch.full((c.b, c.R, 6 + 2 + 2, 64 + 8), float("nan"), dtype=c.dtype, device="cuda")
+    fused[:, :, :6, :64], fused[:, :, 6:8, :64], fused[:, :, 8:, :64] = c.q, c.k_new, c.v_new
+    n = c.k.shape[0]
+    codes = torch.full((3, n, 2, 2, 16, 48), 0x77, dtype=torch.uint8, device="cuda")
+    scales = torch.full((3, n, 16, 2, 2, 3), 255, dtype=torch.uint8, device="cuda")
+    for i in range(2):
+        codes[1, :, i, :, :, :32] = c.codes[i].transpose(1, 2)
+        scales[1, :, :, i, :, 1:] = c.scales[i]
+    wide = torch.full((c.b, c.R, 6, 3, 64), 7.0, dtype=c.dtype, device="cuda")
+    c.packed(out=wide[:, :, :, 1], q=fused[:, :, :6, :64], k_new=fused[:, :, 6:8, :64], v_new=fused[:, :, 8:, :64],
+             k_cache=codes[1, :, 0, :, :, :32].transpose(1, 2), v_cache=codes[1, :, 1, :, :, :32].transpose(1, 2), k_scale=scales[1, :, :, 0, :, 1:],
+             v_scale=scales[1, :, :, 1, :, 1:])
+    c.check(wide[:, :, :, 1].contiguous())
+    assert (wide[:, :, :, 0] == 7).all() and (wide[:, :, :, 2] == 7).all()
+
+
+@pytest.mark.parametrize("scale", [-0.25, 0.0])
+def test_out_may_be_q_and_other_scales(scale):
+    c = PackedCase(4, 1, 64, 16, 3, [80, 700], seed=36)
+    c.v_new[0, 1, 0, 5] = float("inf")       # (the share is gone through twice)
+    c.scale = scale
+    want = c.packed()
+    q = c.q.clone()
+    live = dev(np.arange(c.R)[None] <= c.n_nodes[:, None])
+    c.packed(out=q, q=q)
+    assert torch.equal(q[live], want[live])
+    c = PackedCase(4, 1, 64, 16, 3, [80, 700], seed=37)
+    c.scale = scale
+    c.check(c.packed())
+
+
+@pytest.mark.parametrize("D", [96, 128, 256])
+def test_a_group_that_is_not_a_number_reaches_its_sequence_and_head(D):
+    c = PackedCase(4, 2, D, 16, 3, [90, 200, 33], seed=38)
+    c.scales[1][c.table[1, 3], 5, 1, 2] = 255       # a value of sequence 1, head 1, elements 64 .. 95
+    c.scales[0][c.table[2, 0], 7, 0, 0] = 255       # a key of sequence 2, head 0
+    got = c.packed()
+    for q in range(3):
+        rows = got[q, :c.n_nodes[q] + 1]
+        want = torch.zeros_like(rows, dtype=torch.bool)
+        if q == 1:
+            want[:, 2:, 64:96] = True
+        if q == 2:
+            want[:, :2] = True
+        assert torch.equal(rows.isnan(), want), q
+        assert rows[~want].isfinite().all()
+
+
+def test_keys_whose_products_are_infinite_have_no_weight():
+    """Scales whose largest values are beyond bfloat16, in a head that does not fill its tile: a product of -inf is a weight of zero."""
+    c = PackedCase(1, 1, 96, 16, 0, [70], seed=39)
+    c.q[:] = 1.0
+    c.codes[0][c.table[0, 1], 3] = 0xff             # -6 * 2^127 throughout
+    c.scales[0][c.table[0, 1], 3] = 254
+    c.k_new[:] = 0
+    got = c.packed()
+    assert got.isfinite().all()
+    c.codes[0][c.table[0, 1], 3], c.scales[0][c.table[0, 1], 3] = 0xff, 130     # -48 * 96: no weight either
+    c.values()
+    c.scale = 1.0
+    c.check(c.packed())
+
+
+def test_values_that_are_all_the_same_come_out_as_they_are():
+    c = PackedCase(8, 2, 128, 16, 3, [300, 2, 0, 2000], seed=40)
+    c.codes[1][:], c.scales[1][:], c.v_new[:] = 0x55, 120, 3 * 2.0 ** -7
+    got = c.packed()
+    for q in range(4):
+        assert (got[q, :c.n_nodes[q] + 1] == 3 * 2.0 ** -7).all()
+
+
+def test_two_streams_at_once_and_the_same_bits():
+    a, b = PackedCase(8, 2, 128, 16, 3, [700, 90, 300], seed=41), PackedCase(8, 2, 128, 16, 3, [500, 4000, 0], seed=42)
+    wa, wb = a.packed(), b.packed()
+    a.check(wa)
+    outs = [torch.full(x.q.shape, 7.0, dtype=x.dtype, device="cuda") for x in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    spaces = [a.space(), b.space()]
+    fixed = [dict(block_table=dev(x.table), ctx_len=dev(x.ctx), node_parent=dev(x.parent), n_nodes=dev(x.n_nodes)) for x in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, o, w, f, s in zip((a, b), outs, spaces, fixed, streams):
+            B.spec_packed_attention(x.q, x.k_new, x.v_new, *x.codes, *x.scales, out=o, workspace=w, scale=x.scale, stream=s, **f)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], wa) and torch.equal(outs[1], wb)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    cases = [PackedCase(4, 2, 64, 16, 5, ctx, seed=43 + i) for i, ctx in enumerate(([100, 31, 0], [7, 112, 1600], [112, 1, 2]))]
+    live, pool = cases[0], max(c.k.shape[0] for c in cases)
+    width = max(c.table.shape[1] for c in cases)
+    cache = [torch.zeros((pool, *x.shape[1:]), dtype=torch.uint8, device="cuda") for x in (*live.codes, *live.scales)]
+    table = torch.zeros((3, width), dtype=torch.int32, device="cuda")
+    ctx, parent, count = dev(live.ctx), dev(live.parent), dev(live.n_nodes)
+    q, kn, vn, out, space = live.q.clone(), live.k_new.clone(), live.v_new.clone(), torch.zeros_like(live.q), live.space()
+
+    def load(c):
+        for to, x in zip(cache, (*c.codes, *c.scales)):
+            to[:x.shape[0]] = x
+        table[:, :c.table.shape[1]] = dev(c.table)
+        for to, x in ((ctx, dev(c.ctx)), (parent, dev(c.parent)), (count, dev(c.n_nodes)), (q, c.q), (kn, c.k_new), (vn, c.v_new)):
+            to.copy_(x)
+        out.fill_(7.0)
+
+    load(live)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        B.spec_packed_attention(q, kn, vn, *cache, table, ctx, parent, count, out, space, live.scale)
+    for c in cases + cases[::-1]:
+        load(c)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out)
