@@ -543,9 +543,8 @@ spec_status_t spec_packed_load(const spec_packed_t* cache, int64_t cache_layer_s
                                const spec_rows_t* v_out, void* hip_stream);
 
 /* TREE ATTENTION over a cache of four bits: spec_tree_attention in SPEC_BF16 with the values of the codes in the place of the cached keys
- * and values; everything else is as there, the workspace of spec_packed_attention_workspace() bytes too.  head_dim is a multiple of 32,
- * at most 256.  A group of scale 255 is not a number: it reaches the rows that see its token (all of the sequence's), as any such value
- * does. */
+ * and values; everything else, workspace included, is as there.  head_dim is a multiple of 32, at most 256.  A group of scale 255 is not
+ * a number: it reaches the rows that see its token (all of the sequence's), as any such value does. */
 spec_status_t spec_packed_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new,
                                     const spec_packed_t* cache, const int32_t* block_table, const int32_t* ctx_len,
                                     const int32_t* node_parent, const int32_t* n_nodes, const spec_rows_t* out, int32_t batch,

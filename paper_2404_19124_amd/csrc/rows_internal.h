@@ -34,8 +34,7 @@ struct AttentionJob {
 };
 int64_t attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim, bool bf16);
 hipError_t launch_attention(const AttentionJob& job, bool bf16, hipStream_t st);
-int64_t packed_attention_workspace(int batch, int M, int q_heads, int kv_heads, int head_dim);
-hipError_t launch_packed_attention(const AttentionJob& job, hipStream_t st);
+hipError_t launch_packed_attention(const AttentionJob& job, hipStream_t st);   // workspace: attention_workspace's of bfloat16
 
 // ---- block tables and slot maps --------------------------------------------------------
 struct ExtendJob {

@@ -75,7 +75,7 @@ extern "C" spec_status_t spec_tree_attention_workspace(int32_t batch, int32_t M,
 static spec_status_t check_attention(const spec_rows_t* q, const spec_rows_t* k_new, const spec_rows_t* v_new, const int32_t* block_table,
                                      const int32_t* ctx_len, const int32_t* node_parent, const spec_rows_t* out, int32_t batch, int32_t M,
                                      int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype, int32_t block_size, int32_t max_blocks,
-                                     void* workspace, int64_t workspace_bytes, bool packed) {
+                                     void* workspace, int64_t workspace_bytes) {
   if (!q || !k_new || !v_new || !out || !q->at || !k_new->at || !v_new->at || !out->at || !block_table || !ctx_len)
     return fail(SPEC_EINVAL, "a required pointer is NULL");
   spec_status_t s = check_attention_shape(batch, M, q_heads, kv_heads, head_dim, dtype);
@@ -88,8 +88,7 @@ static spec_status_t check_attention(const spec_rows_t* q, const spec_rows_t* k_
     return fail(SPEC_ESHAPE, "k_new and v_new must have the same strides");
   if (!rows_aligned(*q, esz) || !rows_aligned(*k_new, esz) || !rows_aligned(*v_new, esz) || !rows_aligned(*out, esz))
     return fail(SPEC_EINVAL, "rows of q, k_new, v_new and out must start on multiples of 16 bytes");
-  const int64_t need = packed ? packed_attention_workspace(batch, M, q_heads, kv_heads, head_dim)
-                              : attention_workspace(batch, M, q_heads, kv_heads, head_dim, dtype == SPEC_BF16);
+  const int64_t need = attention_workspace(batch, M, q_heads, kv_heads, head_dim, dtype == SPEC_BF16);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SPEC_EINVAL, "workspace of %lld bytes, needed are %lld", (long long)(workspace ? workspace_bytes : 0), (long long)need);
   if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(SPEC_EINVAL, "workspace must be 16-byte aligned");
@@ -121,7 +120,7 @@ extern "C" spec_status_t spec_tree_attention(const spec_rows_t* q, const spec_ro
                                              int64_t workspace_bytes, void* hip_stream) {
   if (!cache) return fail(SPEC_EINVAL, "a required pointer is NULL");
   spec_status_t s = check_attention(q, k_new, v_new, block_table, ctx_len, node_parent, out, batch, M, q_heads, kv_heads, head_dim, dtype, cache->block_size,
-                                    max_blocks, workspace, workspace_bytes, false);
+                                    max_blocks, workspace, workspace_bytes);
   if (s != SPEC_OK) return s;
   const int esz = element_bytes(dtype);
   s = check_cache(*cache, esz);
@@ -394,7 +393,7 @@ extern "C" spec_status_t spec_packed_attention_workspace(int32_t batch, int32_t 
   spec_status_t s = check_attention_shape(batch, M, q_heads, kv_heads, head_dim, SPEC_BF16);
   if (s != SPEC_OK) return s;
   if (head_dim % 32) return fail(SPEC_ESHAPE, "head_dim = %d must be a multiple of 32", head_dim);
-  *bytes = packed_attention_workspace(batch, M, q_heads, kv_heads, head_dim);
+  *bytes = attention_workspace(batch, M, q_heads, kv_heads, head_dim, true);
   return SPEC_OK;
 }
 
@@ -407,7 +406,7 @@ extern "C" spec_status_t spec_packed_attention(const spec_rows_t* q, const spec_
   spec_status_t s = check_packed(cache, head_dim);
   if (s != SPEC_OK) return s;
   s = check_attention(q, k_new, v_new, block_table, ctx_len, node_parent, out, batch, M, q_heads, kv_heads, head_dim, SPEC_BF16, cache->block_size,
-                      max_blocks, workspace, workspace_bytes, true);
+                      max_blocks, workspace, workspace_bytes);
   if (s != SPEC_OK) return s;
   if (!rows_apart({{batch, out->seq_stride}, {M + 1, out->row_stride}, {q_heads, out->head_stride}}, head_dim))
     return fail(SPEC_EINVAL, "rows of out overlap");

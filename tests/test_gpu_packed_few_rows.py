@@ -1,4 +1,4 @@
-"""spec_packed_attention with up to 16 query rows for a key head, where a kernel of its own takes pages of a multiple of 16 tokens: what may
+"""spec_packed_attention with up to 32 query rows for a key head, where a kernel of its own takes pages of a multiple of 16 tokens: what may
 lie where nothing is read, places out of range, strides, infinities, streams and graphs."""
 import numpy as np
 import pytest

@@ -177,7 +177,7 @@ class Server:
 
 
 @pytest.mark.parametrize("captured", [False, True])
-@pytest.mark.parametrize("H,M", [(2, 9), (8, 9)])    # up to 16 query rows for a key head, and more
+@pytest.mark.parametrize("H,M", [(2, 9), (8, 9)])    # up to 32 query rows for a key head, and more
 def test_steps_against_the_oracles(H, M, captured):
     rng = np.random.default_rng(6)
     prompt = lambda n: [int(t) for t in rng.integers(0, V, n)]
