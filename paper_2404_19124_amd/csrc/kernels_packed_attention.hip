@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_attention_kerne
 // Values pass through memory of the wave's own, 32 keys at a time, to be read transposed.  A wave's next tile is on its way while it works
 // on one; every read of a tile of cached tokens is unconditional, so that none waits for those before it.  Bytes bound it: 64 sequences
 // of up to 8000 tokens, 8 heads of 128, one token with 64 heads each, 308 MB, 80 us, 3.9 TB/s (a sum over as many bytes: 4.0), the tiles of
-// all four waves in turn by barriers 137 us.  Less work: 32 heads, one sequence of 500 tokens 14.7 -> 12.6 us, 32 of 500, 8 heads 24.2 -> 21.6.
+// all four waves in turn by barriers 137 us.  Less work: 32 heads, one sequence of 500 tokens 14.7 -> 12.4 us, 32 of 500, 8 heads 24.2 -> 20.8.
 // Two workgroups to a CU: three of 168 registers 91 us.  A page that is no multiple of 16 tokens keeps the barriers.
 constexpr int kStreamRows = 16, kStreamCost = 12;
 // (the cost: what a unit's start and end take, in tiles.  The call above, where one sequence has nothing cached, with a cost of 2: 106 us, 5: 96,
@@ -177,8 +177,9 @@ struct PackedStream {
   typedef AttentionTile<true, DP, 1, 1> Tile;           // (its queries in another order)
   static constexpr int NC = DP / 32, NS = DP > 128 ? 2 : 1;      // words of codes of a lane's quarter of a key, and scales
   static constexpr int NB = KT / 16, ROWB = DP * 2, SWZ = ROWB / 16 < 16 ? ROWB / 16 - 1 : 15;
-  static constexpr int WAVE = 32 * ROWB, LDS = 4 * WAVE;         // memory of a wave
-  static_assert(3 * 64 * (DP / 4 + 2) * 4 <= LDS, "the waves' results fit their memory");
+  static constexpr int PER = DP / 4 + 2;                         // results of a lane
+  static constexpr int WAVE = PER * 256, LDS = 4 * WAVE;         // memory of a wave: its values, or its results
+  static_assert(32 * ROWB <= WAVE, "values of 32 keys");
   const AttentionJob& p;
   int64_t to_v_rows;
   int last_word;                                        // of a row of bfloat16
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(A
   typedef typename Stream::Tile Tile;
   constexpr int BM = kStreamRows, NB = Stream::NB, NC = Stream::NC, ND = DP / 16, ROWB = Stream::ROWB;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  __shared__ uint32_t s_again;
+  __shared__ int s_odd[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, grp = lane >> 4;
   const int G = p.q_heads / p.kv_heads;
   Schedule<BM, kStreamCost> plan = {p, G};
@@ -310,16 +311,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(A
   uint16_t* s_up = reinterpret_cast<uint16_t*>(smem + Stream::LDS);
   lds_u8* vb = (lds_u8*)smem + wave * Stream::WAVE;
   bool careful = false;        // the second pass over this share
-  int n_units = 0, first_odd = 1 << 30, unit0 = 0;   // as in attention_body
-  if (tid == 0) s_again = 0;
+  int n_units = 0, first_odd = 1 << 30, unit0 = 0;   // as in attention_body (of all waves: they have the same rows)
   while (more) {
     const int rows = (now.nodes + 1) * G - now.block * BM;
     const bool holds_rows = (now.tile0 + now.n_tiles) * KT > now.ctx;
-    if (holds_rows)
-      for (int i = tid; i < now.keys - now.ctx - 1; i += 256) {
-        const int up = p.node_parent[(int64_t)now.q * p.M + i];
-        s_up[i + 1] = (uint16_t)(up >= 0 && up < i ? up + 1 : 0);
-      }
+    const int n_up = holds_rows ? now.keys - now.ctx - 1 : 0;
+    int up = tid < n_up ? p.node_parent[(int64_t)now.q * p.M + tid] : 0;   // (on its way with the queries and the places)
     Tile x;
     const int mm = l16 < rows ? now.block * BM + l16 : 0;
     x.row_of[0] = mm / G;
@@ -341,6 +338,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(A
     in.of(now);
     const int n_tiles = uniform(now.n_tiles);
     typename Stream::Places f = in.places(now, 0);
+    for (int i = tid; i < n_up; i += 256) {
+      s_up[i + 1] = (uint16_t)(up >= 0 && up < i ? up + 1 : 0);
+      if (i + 256 < n_up) up = p.node_parent[(int64_t)now.q * p.M + i + 256];
+    }
     typename Stream::Codes kc, vc;
     uint64_t cached = 0;
     bool odd = false;
@@ -473,72 +474,61 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_stream_kernel(A
     }
     l_run = groups_sum(l_run);
 
-    // ---- join of the waves ----
-    float* box = reinterpret_cast<float*>(smem);
-    constexpr int PER = DP / 4 + 2;
-    odd = __syncthreads_or(odd);
-    if (wave > 0) {
-      float* to = box + (wave - 1) * PER * 64 + lane;
-      to[0] = m_run;
-      to[64] = l_run;
+    // ---- join of the waves: each one joins a quarter of the head ----
+    auto mine_is = [&](int d) { return d / (ND / 4) == wave; };
+    float* box = reinterpret_cast<float*>(smem) + lane;
+    constexpr int PER = Stream::PER;
+    box[wave * PER * 64] = m_run;
+    box[(wave * PER + 1) * 64] = l_run;
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[(2 + d * 4 + i) * 64] = x.o[0][d][i];
-    }
+      for (int i = 0; i < 4; ++i) box[(wave * PER + 2 + d * 4 + i) * 64] = x.o[0][d][i];
+    if (lane == 0) s_odd[wave] = odd;
     __syncthreads();
+    float part[4];
+    m_run = kLowest, l_run = 0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) part[y] = box[y * PER * 64], m_run = fmaxf(m_run, part[y]);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) part[y] = __builtin_amdgcn_exp2f(part[y] - m_run), l_run = __builtin_fmaf(box[(y * PER + 1) * 64], part[y], l_run);
+    bool finite = true;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+      if (mine_is(d)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float o = 0;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o = __builtin_fmaf(box[(y * PER + 2 + d * 4 + i) * 64], part[y], o);
+          x.o[0][d][i] = o;
+          finite = finite && o * 0.0f == 0.0f;
+        }
+      }
     const bool whole = now.n_seg == now.tiles;
     if (!whole && now.tile0 == 0) mine = {now.q, now.g, now.block, plan.last(), min(rows, BM)};
-    if (wave == 0) {
-      for (int y = 0; y < 3; ++y) {
-        const float* of = box + y * PER * 64 + lane;
-        const float m = of[0], m_new = fmaxf(m, m_run);
-        const float ours = __builtin_amdgcn_exp2f(m_run - m_new), its = __builtin_amdgcn_exp2f(m - m_new);
-        m_run = m_new;
-        l_run = l_run * ours + of[64] * its;
+    if (!careful && (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]) && __syncthreads_or(!finite)) first_odd = min(first_odd, n_units);
+    if (careful && holds_rows)
+      add_left_out(x, now.k_rows, in.to_v_rows, p.new_row, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, s_up, in.last_word);
+    if (l16 < rows && (careful ? n_units - unit0 >= first_odd : n_units < first_odd)) {
+      const float inv = whole ? 1.0f / l_run : 1.0f;
+      uint8_t* out = static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)x.row_of[0] * p.out_row + (int64_t)(now.g * G + mm % G) * p.out_head;
+      float* to = ws.part + ((int64_t)(me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + l16) * (DP + 4);
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x.o[0][d][i] = x.o[0][d][i] * ours + of[(2 + d * 4 + i) * 64] * its;
+      for (int d = 0; d < ND; ++d) {
+        const int e = d * 16 + grp * 4;
+        if (!mine_is(d)) continue;
+        const f32x4 v = x.o[0][d] * inv;
+        if (!whole) *reinterpret_cast<f32x4*>(to + e) = v;
+        else if (e < p.head_dim) *reinterpret_cast<uint64_t*>(out + e * 2) = (uint64_t)f32_to_bf16_pair(v[2], v[3]) << 32 | f32_to_bf16_pair(v[0], v[1]);
       }
-      if (odd && !careful) {
-        float zero = 0;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x.o[0][d][i], 0.0f, zero);
-        if (__any(!(zero == 0.0f))) {
-          if (lane == 0) s_again = 1;
-          first_odd = min(first_odd, n_units);
-        }
-      }
-      if (careful && holds_rows)
-        add_left_out(x, now.k_rows, in.to_v_rows, p.new_row, now.ctx, now.tile0 * KT, (now.tile0 + now.n_tiles) * KT, s_up, in.last_word);
-      if (l16 < rows && (careful ? n_units - unit0 >= first_odd : n_units < first_odd)) {
-        if (whole) {
-          const float inv = 1.0f / l_run;
-          uint8_t* to = static_cast<uint8_t*>(p.out) + now.q * p.out_seq + (int64_t)x.row_of[0] * p.out_row + (int64_t)(now.g * G + mm % G) * p.out_head;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const int e = d * 16 + grp * 4;
-            if (e < p.head_dim) {
-              const f32x4 v = x.o[0][d] * inv;
-              *reinterpret_cast<uint64_t*>(to + e * 2) = (uint64_t)f32_to_bf16_pair(v[2], v[3]) << 32 | f32_to_bf16_pair(v[0], v[1]);
-            }
-          }
-        } else {
-          float* to = ws.part + ((int64_t)(me * 2 + (now.tile0 == 0 ? 1 : 0)) * BM + l16) * (DP + 4);
-#pragma unroll
-          for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + d * 16 + grp * 4) = x.o[0][d];
-          if (grp == 0) to[DP] = m_run, to[DP + 1] = l_run;
-        }
-      }
+      if (!whole && wave == 0 && grp == 0) to[DP] = m_run, to[DP + 1] = l_run;
     }
     more = plan.following(now);
     if (more) plan.advance(now);
     ++n_units;
-    __syncthreads();   // the results and the parents have been read
-    if (!more && !careful && s_again) {
+    if (careful) __syncthreads();   // the parents have been read
+    if (!more && !careful && first_odd < n_units) {
       careful = true;
       unit0 = n_units;
       more = plan.first(now);
@@ -591,7 +581,7 @@ static hipError_t launch_stream_t(const AttentionJob& job, const AttentionPlan& 
 }
 
 // The streams' plan (no more workspace than the other's); bm 0: too many query rows for a key/value head.  More than 16 of them are two units, which read the same keys beside each
-// other: 17 rows of 32 heads, 11 sequences of up to 6100 tokens 99 -> 60 us, 32 rows of 8 heads, 16 of 4000 39 -> 29; but three and four
+// other: 17 rows of 40 heads, 6 sequences of up to 9600 tokens 110 -> 64 us, 32 rows of 8 heads, 16 of 4000 39 -> 29; but three and four
 // units 42 -> 46 us (48 rows, 8 heads, 32 of 2000) and 73 -> 83 (49 rows, 32 heads, 16 of 2000).
 static AttentionPlan plan_streams(int M, int q_heads, int kv_heads, int head_dim) {
   AttentionPlan a = plan_attention(M, q_heads, kv_heads, head_dim, true);
