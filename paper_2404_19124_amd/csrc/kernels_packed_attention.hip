@@ -1,8 +1,8 @@
 // Attention of a token tree's rows over a paged cache of four bits and their own ancestors.  The mathematics, the shares, the softmax and
 // the products are those of the attention over a cache of 16 bits (attention_body.h); a tile's codes pass through registers on their way
 // into LDS, where they lie as the bfloat16 values that they stand for: every value is one, so nothing is rounded.  With many query rows the
-// products bound it: 32 sequences of 8 key/value heads with 520 rows each, 225 us, 570 TFLOP/s, the time that the cache of 16 bits takes,
-// whose tiles are worked on in the same way.  With few rows it is the reading: see the second kernel.
+// products bound it: 32 sequences of 8 key/value heads with 520 rows each, 225 us, 570 TFLOP/s (a cache of 16
+// bits, whose tiles are worked on in the same way: 248).  With few rows it is the reading: see the second kernel.
 #include <atomic>
 
 #include "attention_body.h"
