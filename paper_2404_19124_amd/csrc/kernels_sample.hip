@@ -179,8 +179,8 @@ __device__ __forceinline__ SamplePart take_run(const void* row, int begin, int r
         for (int c = 0; c < path.n; ++c) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            // (what was emitted before counts where its bit is set; here it is taken into account so that the bit can be)
-            if (path.tok[c] - first == j) x.c[j / 8][j % 8] = (pen.seen && !((x.seen >> j) & 1) ? 0 : x.c[j / 8][j % 8]) + 1, x.seen |= 0x10000u << j;
+            // (what was emitted before counts where its bit is set, bit j; a token that the path has had has bit 16 + j, and its count goes on)
+            if (path.tok[c] - first == j) x.c[j / 8][j % 8] = (pen.seen && !((x.seen >> j) & 0x10001u) ? 0 : x.c[j / 8][j % 8]) + 1, x.seen |= 0x10000u << j;
           }
         }
       }
