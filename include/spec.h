@@ -466,7 +466,8 @@ spec_status_t spec_verify_sampled(const void* logits, int32_t logits_dtype, cons
                                   int32_t* counts_out, uint32_t* seen_out, void* workspace, int64_t workspace_bytes,
                                   void* hip_stream);
 
-/* Bytes of workspace such a call needs (host-only). */
+/* Bytes of workspace such a call needs (host-only); with the same vocab no less for a larger batch or M, so that one buffer of the
+ * largest call's size serves all. */
 spec_status_t spec_verify_sampled_workspace(int32_t batch, int32_t M, int32_t vocab, int32_t logits_dtype, int64_t* bytes);
 
 /* ---- rotation and norms of heads, and a cache of four bits ----------------------------------------------------

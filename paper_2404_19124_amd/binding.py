@@ -849,7 +849,7 @@ def spec_verify_tree(logits: torch.Tensor, cand_tokens: torch.Tensor, cand_node:
 
 
 def spec_verify_sampled_workspace(batch: int, R: int, vocab: int, dtype: torch.dtype) -> int:
-    """Bytes of workspace of spec_verify_sampled on logits [batch, R, vocab] (host-only: needs no GPU)."""
+    """Bytes of workspace of spec_verify_sampled on logits [batch, R, vocab] (host-only: needs no GPU); no less for a larger batch or R."""
     out = C.c_int64()
     _check(lib().spec_verify_sampled_workspace(int(batch), int(R) - 1, int(vocab), _DTYPE_CODE.get(dtype, -1), C.byref(out)))
     return int(out.value)

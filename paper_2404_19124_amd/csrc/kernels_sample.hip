@@ -611,7 +611,9 @@ static SamplePlan plan_sample(int batch, int M, int V) {
   a.span = a.run * kSampleThreads;
   a.parts = (int)(((int64_t)V + a.span - 1) / a.span);
   auto padded = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
-  a.part_bytes = padded((a.all_rows ? rows : 2 * (int64_t)batch) * a.parts * sizeof(SamplePart));
+  // no less than fewer sequences or rows need, whose partials may all be held at once: the largest call's buffer serves the others
+  const int64_t held = max(max((int64_t)batch, min(rows, kAllRowsLogits / V)), a.all_rows ? (int64_t)0 : 2 * (int64_t)batch);
+  a.part_bytes = padded(held * a.parts * sizeof(SamplePart));
   a.node_bytes = padded((int64_t)batch * M * sizeof(float));
   a.slot_bytes = padded((int64_t)batch * (kMaxStages + 2) * sizeof(SampleSlot));
   return a;
