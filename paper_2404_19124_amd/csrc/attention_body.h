@@ -241,6 +241,8 @@ struct AttentionTile {
           if constexpr (!BF16) l_run[mq] += w;
         }
     }
+    // The weights are rounded to bfloat16 for their product with the values, since products of float32 run at an eighth of the rate.  That adds to
+    // the rounding of the result: off from 64 bits by 1.60e-3 to 1.70e-3 relative, 1.57e-3 to 1.61e-3 with float32 weights.
     // (the sum is that of the weights as they are multiplied: equal values come out as they are, whatever the rounding)
     auto sum = [&](int mq, uint32_t pair) {
       const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};

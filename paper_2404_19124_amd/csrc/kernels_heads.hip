@@ -224,8 +224,9 @@ __device__ __forceinline__ uint32_t pack_group(const float (&x)[8], uint32_t& co
 }
 
 // A lane takes a word of a head, eight elements, four lanes a group of 32: a wave reads 1 KiB and writes 256 bytes in a row.  The other
-// elements of its pairs it reads again, from the cache where its neighbours' reads have brought them.  Memory bounds it: 16,000 tokens of 8
-// heads of 128 with their norms, rotation and tables, 91 MB, 26 us, 3.5 TB/s (a whole group to a lane, 64 bytes apart: 53 us).
+// elements of its pairs it reads again, from the cache where its neighbours' reads have brought them, and norms and turns them too: 16,000
+// tokens of 8 heads of 128 with their norms, rotation and tables, 91 MB, 26 us, 3.5 TB/s (a whole group to a lane, 64 bytes apart: 53 us).  Vector
+// instructions take 63 % of the SIMDs' time and 48 % of the waves' is waiting: both bound it (rows into a cache of 16 bits: 28 and 71 %, 5.0 TB/s).
 template <bool PAIRS>
 __global__ __launch_bounds__(256) void pack_kernel(PackJob p) {
   typedef HeadWord<true> Word;

@@ -164,13 +164,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_attention_kerne
 // tiles of a segment go round the four waves, which meet at its end only.  Keys go from codes to the operand of the first product in
 // registers: lane l16 of group grp holds elements grp * DP/4 on of key l16 of a block of 16, and the queries lie in that order too.
 // Values pass through memory of the wave's own, 32 keys at a time, to be read transposed.  A wave's next tile is on its way while it works
-// on one; every read of a tile of cached tokens is unconditional, so that none waits for those before it.  Bytes bound it: 64 sequences
-// of up to 8000 tokens, 8 heads of 128, one token with 64 heads each, 308 MB, 80 us, 3.9 TB/s (a sum over as many bytes: 4.0), the tiles of
-// all four waves in turn by barriers 137 us.  Less work: 32 heads, one sequence of 500 tokens 14.7 -> 12.4 us, 32 of 500, 8 heads 24.2 -> 20.8.
-// Two workgroups to a CU: three of 168 registers 91 us.  A page that is no multiple of 16 tokens keeps the barriers.
+// on one; every read of a tile of cached tokens is unconditional, so that none waits for those before it.  64 sequences
+// of up to 8000 tokens, 8 heads of 128, one token with 64 heads each, 308 MB, 80 us, 3.9 TB/s, the tiles of
+// all four waves in turn by barriers 137 us.  Half of the waves' time is waiting, vector instructions take 32 % of the SIMDs':
+// it is not the memory's rate that bounds it (the same call over 16 bits reads 5.0 TB/s).  Every second load fetches one byte of scale to a lane.
+// Less work: 32 heads, one sequence of 500 tokens 14.7 -> 12.4 us, 32 of 500, 8 heads 24.2 -> 20.8.
+// Two workgroups to a CU: three of 168 registers 91 us.  A page that is no multiple of 16 tokens keeps the barriers: pages of 50 in the call above 157 us.
+// Where the heads of a token lie beside each other, a head's rows 64 bytes each far apart, it takes 122 us (head by head in a block: 80).
 constexpr int kStreamRows = 16, kStreamCost = 12;
-// (the cost: what a unit's start and end take, in tiles.  The call above, where one sequence has nothing cached, with a cost of 2: 106 us, 5: 96,
-// 8: 84, 12 and 18: 80)
+// (the cost: what a unit's start and end take, in tiles.  The call above, where one sequence has nothing cached, with costs of 2, 6, 12 and 20:
+// 103, 88, 80 and 81 us; 8 such sequences 46, 29, 24 and 26; one of 30,000 tokens 30, 30, 30 and 29; 17 rows of 40 heads, 6 sequences 119, 67, 54 and 55; 32
+// rows of 8 heads, 16 sequences 55, 34, 31 and 32)
 typedef __attribute__((address_space(1))) uint8_t global_u8;
 template <int DP>
 struct PackedStream {
@@ -581,7 +585,8 @@ static hipError_t launch_stream_t(const AttentionJob& job, const AttentionPlan& 
 }
 
 // The streams' plan (no more workspace than the other's); bm 0: too many query rows for a key/value head.  More than 16 of them are two units, which read the same keys beside each
-// other: 17 rows of 40 heads, 6 sequences of up to 9600 tokens 110 -> 64 us, 32 rows of 8 heads, 16 of 4000 39 -> 29; but three and four
+// other: 17 rows of 40 heads, 6 sequences of up to 9600 tokens 92 -> 54 us (their bytes at a sum's rate: 43), 32 rows of 8 heads, 16 of up to 4000 44 -> 31 (10);
+// but three and four
 // units 42 -> 46 us (48 rows, 8 heads, 32 of 2000) and 73 -> 83 (49 rows, 32 heads, 16 of 2000).
 static AttentionPlan plan_streams(int M, int q_heads, int kv_heads, int head_dim) {
   AttentionPlan a = plan_attention(M, q_heads, kv_heads, head_dim, true);

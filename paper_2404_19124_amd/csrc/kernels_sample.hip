@@ -592,9 +592,12 @@ __global__ __launch_bounds__(kSampleThreads, 3) void sample_walk_kernel(SampleJo
   if (tid < 64) emit(p, q, s, token, weight, s_set.sum);
 }
 
-// Up to so many logits are all taken in one launch, more row by row down the paths, a launch for each depth.  All rows / paths, us: trees of
-// 49 rows, vocabulary 32,000, float32, 1, 8, 16 and 32 sequences (1.6, 13, 25 and 50 million logits) 24.5 / 30.6, 42.4 / 58.4, 60.6 / 65.1 and
-// 95.2 / 68.5; of 65 rows, 128,256, bfloat16, 1, 2, 4 and 8 sequences (8, 17, 33 and 67 million) 37.1 / 43.9, 49.1 / 47.1, 70.0 / 51.9 and 111 / 65.0.
+// Up to so many logits are all taken in one launch, more row by row down the paths, a launch for each depth.  All rows / paths, us, where
+// half of the drafted tokens or more are kept: trees of 49 rows, vocabulary 32,000, float32, 4, 8, 12, 16 and 32 sequences (6, 13, 19, 25 and 50
+// million logits) 35.8 / 55.2, 43.6 / 60.8, 53.0 / 62.4, 63.6 / 63.6 and 100 / 69; of 65 rows, 128,256, bfloat16, 1, 2, 3, 4 and 8 sequences (8, 17, 25, 33
+// and 67 million) 36.2 / 52.6, 48.9 / 61.2, 62.4 / 64.5, 73.8 / 66.2 and 121 / 73; of 97 rows, 32,000, bfloat16, 4, 8 and 16 (12, 25 and 50 million) 40.6 / 60.8,
+// 55.4 / 60.6 and 85.5 / 65.2.  So they meet between 25 and 30 million in either type, and from here to there the paths cost up to 9 us more; where
+// paths end early they are faster, and all rows are not.
 constexpr int64_t kAllRowsLogits = 1 << 24;
 
 struct SamplePlan {
