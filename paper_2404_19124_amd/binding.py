@@ -1048,7 +1048,8 @@ def spec_packed_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Ten
 
     One layer: k_new, v_new [rows, kv_heads, head_dim]; k_cache, v_cache [n_blocks, block_size, kv_heads, head_dim / 2] uint8, rows on 16
     bytes; k_scale, v_scale [n_blocks, block_size, kv_heads, head_dim / 32] uint8: any strides but along the last dimension, the same in
-    k_* and v_* (attention is fastest on views of [n_blocks, kv_heads, block_size, ...], a head's tokens one behind the other).  Several layers at once: a first dimension of layers in all six.  The others as for spec_cache_append."""
+    k_* and v_* (attention is fastest on views of [n_blocks, kv_heads, block_size, ...], a head's tokens one behind the other).  Several layers
+    at once: a first dimension of layers in all six.  The others as for spec_cache_append."""
     if _CHECK_DEVICE and _done((_fast or _native()).packed_append(
             k_new, v_new, slot, k_cache, v_cache, k_scale, v_scale, src_row, pos, cos, sin, k_weight, eps, pairs, stream)):
         return

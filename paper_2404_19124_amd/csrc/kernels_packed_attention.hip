@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void packed_attention_kerne
 // it is not the memory's rate that bounds it (the same call over 16 bits reads 5.0 TB/s).  Every second load fetches one byte of scale to a lane.
 // Less work: 32 heads, one sequence of 500 tokens 14.7 -> 12.4 us, 32 of 500, 8 heads 24.2 -> 20.8.
 // Two workgroups to a CU: three of 168 registers 91 us.  A page that is no multiple of 16 tokens keeps the barriers: pages of 50 in the call above 157 us.
-// Where the heads of a token lie beside each other, a head's rows 64 bytes each far apart, it takes 122 us (head by head in a block: 80).
+// Where the heads of a token lie beside each other in a block, not the tokens of a head, so that a head's rows of 64 bytes are apart, it takes 122 us.
 constexpr int kStreamRows = 16, kStreamCost = 12;
 // (the cost: what a unit's start and end take, in tiles.  The call above, where one sequence has nothing cached, with costs of 2, 6, 12 and 20:
 // 103, 88, 80 and 81 us; 8 such sequences 46, 29, 24 and 26; one of 30,000 tokens 30, 30, 30 and 29; 17 rows of 40 heads, 6 sequences 119, 67, 54 and 55; 32
